@@ -298,6 +298,134 @@ int score_candidates_static(const tx_kv_cache* cache, int32_t n_req, const int32
                             const void* serving, const int64_t* serving_offsets /* host */, const void* candidates,
                             const int64_t* candidate_offsets /* host */, float* scores, hipStream_t stream);
 
+/* ------------------------------------------------------------ training */
+
+/* Operators of a training step around score_events: the attention of the
+ * behavior encoder (Sec. 4.1.1) and of the event-sliced decoding (Sec. 4.2)
+ * over packed rows instead of cache pages, and a loss on the action head's
+ * logits (Sec. 4.1.3), each forward and backward. They need no model or cache:
+ * a call takes its tensors, host offsets, a workspace (256-byte aligned, at
+ * least the bytes its size function gives; its contents mean nothing between
+ * calls, so a backward call may use another one than its forward) and a
+ * stream of the current device, on which all its tensors live. A call reads
+ * its host arrays before it returns, never synchronises, allocates no device
+ * memory and may be captured into a graph; calls that run at the same time need
+ * workspaces of their own. The same inputs give the same bits, eager or
+ * replayed. Checks and errors as above: TX_E_INVALID, TX_E_UNSUPPORTED and
+ * TX_E_NOMEM (workspace too small) before anything is launched, TX_E_HIP. */
+
+typedef struct {
+  int32_t dtype;           /* tx_dtype of every tensor but the fp32 statistics */
+  int32_t n_heads;         /* query heads */
+  int32_t n_kv_heads;      /* key/value heads, a divisor of n_heads: query head h reads key head
+                              h / (n_heads / n_kv_heads), whose gradient sums over its query heads */
+  int32_t d_head;          /* 32, 64 or 128 (TX_E_UNSUPPORTED otherwise) */
+  int32_t rel_pos_buckets; /* R of tx_rel_attn_* (0 .. 2048; 0 = no bias); 0 for tx_event_attn_* */
+  float scale;             /* logit scale, > 0; 0 = 1 / sqrt(d_head) */
+} tx_attn_config;
+
+/* Element f of row r and head h at data[r * row_stride + h * head_stride + f]
+ * (strides in elements), so heads side by side in a row, a slice of a fused
+ * projection's rows and [head][row][d_head] are all accepted. data and both
+ * strides in bytes must be multiples of 16, strides not negative, a row stride
+ * at most 16 MiB. Rows and heads of a tensor that a call writes must not
+ * overlap, nor overlap anything else the call reads or writes. */
+typedef struct {
+  void* data;
+  int64_t row_stride, head_stride;
+} tx_rows;
+
+/* tx_rel_attn_forward -- causal self-attention of packed sequences with the
+ * encoder's learned relative position bias: sequence i owns rows offsets[i] ..
+ * offsets[i+1]-1 (it may have none), and within it
+ *   t_ij = scale q_i . k_j + rel[h][min(i - j, R - 1)]  for j <= i
+ *   out_i = softmax_j(t_ij) v_j,  lse[h * lse_stride + row] = log sum_j exp t_ij
+ * rel: device [n_heads][R] (null when R = 0). A bias of -1e30 or less masks its
+ * distances, whatever the keys and values there hold; a row with every distance
+ * masked gives out 0 and lse -inf, and its gradients are 0. lse_stride >=
+ * offsets[n_seq]. Rows outside the offsets are neither read nor written.
+ * bf16: products on bf16 with fp32 sums, softmax in fp32, the probabilities
+ * rounded to bf16 for the product with v. */
+size_t tx_rel_attn_workspace_bytes(const tx_attn_config* cfg, int32_t backward, int32_t n_seq,
+                                   const int64_t* offsets /* host */);
+int tx_rel_attn_forward(const tx_attn_config* cfg, int32_t n_seq, const int64_t* offsets /* host */,
+                        const tx_rows* q, const tx_rows* k, const tx_rows* v, const void* rel, const tx_rows* out,
+                        float* lse, int64_t lse_stride, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* tx_rel_attn_backward -- gradients for d_out, given the forward's inputs, out
+ * and lse: d_q, d_k, d_v (rows of the offsets written whole) and d_rel, device
+ * [n_heads][R] in the tensors' type (written, not added to; null when R = 0):
+ * bucket b gets the sum of P_ij (d_out_i . v_j - d_out_i . out_i) over its pairs. */
+int tx_rel_attn_backward(const tx_attn_config* cfg, int32_t n_seq, const int64_t* offsets /* host */,
+                         const tx_rows* q, const tx_rows* k, const tx_rows* v, const void* rel, const tx_rows* out,
+                         const float* lse, int64_t lse_stride, const tx_rows* d_out, const tx_rows* d_q,
+                         const tx_rows* d_k, const tx_rows* d_v, void* d_rel, void* ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* tx_event_attn_forward -- cross-attention of event-sliced decoding: user u
+ * owns key rows key_offsets[u] .. key_offsets[u+1]-1 (its encoded history, any
+ * length) and events event_offsets[u] .. event_offsets[u+1]-1; event e owns
+ * query rows query_offsets[e] .. query_offsets[e+1]-1, each of which sees the
+ * first prefix_len[e] (0 .. the user's length) key rows of its user, whatever
+ * the later rows hold. A prefix of 0 gives out 0, lse -inf and gradients of 0.
+ * n_users + 1 key and event offsets, event_offsets[0] = 0, event_offsets[n_users]
+ * + 1 query offsets, event_offsets[n_users] prefixes. Otherwise as
+ * tx_rel_attn_forward, without bias. */
+size_t tx_event_attn_workspace_bytes(const tx_attn_config* cfg, int32_t backward, int32_t n_users,
+                                     const int64_t* key_offsets /* host */, const int64_t* event_offsets /* host */,
+                                     const int64_t* query_offsets /* host */, const int64_t* prefix_len /* host */);
+int tx_event_attn_forward(const tx_attn_config* cfg, int32_t n_users, const int64_t* key_offsets /* host */,
+                          const int64_t* event_offsets /* host */, const int64_t* query_offsets /* host */,
+                          const int64_t* prefix_len /* host */, const tx_rows* q, const tx_rows* k, const tx_rows* v,
+                          const tx_rows* out, float* lse, int64_t lse_stride, void* ws, size_t ws_bytes,
+                          hipStream_t stream);
+
+/* tx_event_attn_backward -- gradients for d_out. d_k and d_v sum over every
+ * event of the user; key rows that no event sees get zeros. */
+int tx_event_attn_backward(const tx_attn_config* cfg, int32_t n_users, const int64_t* key_offsets /* host */,
+                           const int64_t* event_offsets /* host */, const int64_t* query_offsets /* host */,
+                           const int64_t* prefix_len /* host */, const tx_rows* q, const tx_rows* k,
+                           const tx_rows* v, const tx_rows* out, const float* lse, int64_t lse_stride,
+                           const tx_rows* d_out, const tx_rows* d_q, const tx_rows* d_k, const tx_rows* d_v, void* ws,
+                           size_t ws_bytes, hipStream_t stream);
+
+/* Preference loss of paired answers. An answer is the feedback on one slate:
+ * rows of logits over n_actions actions, one observed action each, whose log
+ * probabilities add up (Sec. 4.1.3, parallel action decoding). Answer 2p is
+ * the preferred one of pair p, answer 2p + 1 the other:
+ *   logp[a] = sum over rows of log softmax(logits[row])[actions[row]]
+ *   m = beta ((logp[2p] - ref_logp[2p]) - (logp[2p+1] - ref_logp[2p+1]))
+ *   loss[p] = -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) */
+typedef struct {
+  int32_t dtype;     /* tx_dtype of logits and d_logits */
+  int32_t n_actions; /* >= 2; 1 = the scalar head's logit s, read as logits [0, s] */
+  float beta;        /* finite */
+  float smoothing;   /* 0 .. 1 */
+} tx_preference_config;
+
+size_t tx_preference_workspace_bytes(const tx_preference_config* cfg, int32_t n_pairs,
+                                     const int64_t* offsets /* host */);
+
+/*   offsets      host [2 n_pairs + 1]: rows of the answers (an answer may have none: logp 0)
+ *   logits       device [rows][row_stride], row_stride >= n_actions elements, any alignment of the type
+ *   actions      device int32 [rows]; a row whose action lies outside 0 .. n_actions-1 (0 .. 1 for the
+ *                scalar head) got no feedback: it adds nothing and its gradient is 0. So does a row whose
+ *                logits are all -inf
+ *   ref_logp     device fp32 [2 n_pairs], the reference model's logp of the same answers; null = 0
+ *   loss, logp   device fp32 [n_pairs], [2 n_pairs]
+ *   row_lse      device fp32 [rows up to offsets[2 n_pairs]]: log sum exp of each row, for the backward call */
+int tx_preference_forward(const tx_preference_config* cfg, int32_t n_pairs, const int64_t* offsets /* host */,
+                          const void* logits, int64_t row_stride, const int32_t* actions, const float* ref_logp,
+                          float* loss, float* logp, float* row_lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* d_logits (rows of the offsets written whole, d_row_stride elements apart,
+ * apart from logits) for d_loss, device fp32 [n_pairs], given the forward's
+ * inputs, logp and row_lse. */
+int tx_preference_backward(const tx_preference_config* cfg, int32_t n_pairs, const int64_t* offsets /* host */,
+                           const void* logits, int64_t row_stride, const int32_t* actions, const float* ref_logp,
+                           const float* logp, const float* row_lse, const float* d_loss, void* d_logits,
+                           int64_t d_row_stride, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------ measurement */
 
 /* Per-kernel timing for roofline reports. While enabled, every kernel launch

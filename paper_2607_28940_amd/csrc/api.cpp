@@ -17,6 +17,7 @@
 #pragma GCC visibility pop
 
 #include "tx_internal.h"
+#include "api_internal.h"
 #include "xplan.h"
 #include "meta_put.h"
 
@@ -25,8 +26,9 @@ using namespace tx;
 // ------------------------------------------------------------------ errors
 namespace {
 thread_local std::string g_err;
+}  // namespace
 
-int fail(int code, const char* fmt, ...) {
+int tx::fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -36,38 +38,11 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-#define TX_HIP(expr)                                                                        \
-  do {                                                                                      \
-    hipError_t e_ = (expr);                                                                 \
-    if (e_ != hipSuccess) return fail(TX_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-#define TX_CHECK(code)           \
-  do {                           \
-    int c_ = (code);             \
-    if (c_ != TX_OK) return c_;  \
-  } while (0)
-
-size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
-
+namespace {
 // Pinned staging per ring slot reserved when a cache is created: the largest
 // per-pass metadata score_candidates_static uploads (its passes are planned
 // to fit).
 constexpr size_t kStagingReserve = 512 << 10;
-
-// Lays sub-buffers out in one device region (256-byte aligned); with a null
-// base it only measures.
-struct Carver {
-  char* base;
-  size_t off = 0;
-  explicit Carver(void* b) : base((char*)b) {}
-  template <class P>
-  P take(size_t bytes) {
-    const size_t o = align_up(off);
-    off = o + bytes;
-    return base ? (P)(base + o) : (P) nullptr;
-  }
-};
 }  // namespace
 
 // ------------------------------------------------------------------ model
@@ -567,15 +542,12 @@ int tx_kv_cache_export(const tx_kv_cache* c, int32_t id, int32_t part, int32_t l
 
 // ------------------------------------------------------------------ kernel timing
 namespace {
-enum KClass {
-  K_GEMM_QKV, K_GEMM_O, K_GEMM_XQ, K_GEMM_XO, K_GEMM_FFN1, K_GEMM_FFN2, K_SELF_ATTN, K_CROSS_ATTN, K_LAYERNORM,
-  K_LN_SCORE, K_COPY, K_ENC_GEMM, K_ENC_ATTN, K_ENC_LAYERNORM, K_SCATTER, K_XKV_GEMM, K_POOL, K_COUNT
-};
 const char* const kClassNames[K_COUNT] = {
     "score.gemm_qkv", "score.gemm_self_out", "score.gemm_cross_q", "score.gemm_cross_out", "score.gemm_ffn_up",
     "score.gemm_ffn_down", "score.self_attention", "score.cross_attention", "score.layernorm", "score.layernorm_score",
     "score.input_copy", "encode.gemm", "encode.causal_attention", "encode.layernorm", "encode.scatter_kv",
-    "encode.gemm_cross_kv", "encode.global_pool"};
+    "encode.gemm_cross_kv", "encode.global_pool", "train.attention_forward", "train.attention_dq",
+    "train.attention_dkv", "train.preference"};
 
 // Records a HIP event pair around each launch on the launching stream while
 // enabled; totals are folded in when read.
@@ -643,29 +615,18 @@ struct Profiler {
 };
 Profiler g_prof;
 
-struct ProfScope {
-  int cls;
-  hipStream_t st;
-  double fl, by;
-  hipEvent_t a = nullptr;
-  ProfScope(int c, hipStream_t s, double f, double b) : cls(c), st(s), fl(f), by(b) {
-    if (g_prof.on && ((g_prof.mask >> c) & 1) && (a = g_prof.get())) (void)hipEventRecord(a, st);
-  }
-  ~ProfScope() {
-    if (!a) return;
-    hipEvent_t b = g_prof.get();
-    if (!b) return;
-    (void)hipEventRecord(b, st);
-    g_prof.recs.push_back({cls, a, b, fl, by});
-  }
-};
 }  // namespace
 
-#define TX_LAUNCH(cls, fl, by, expr) \
-  do {                               \
-    ProfScope ps_((cls), st, (fl), (by)); \
-    TX_HIP(expr);                    \
-  } while (0)
+tx::ProfScope::ProfScope(int c, hipStream_t s, double f, double b) : cls(c), st(s), fl(f), by(b) {
+  if (g_prof.on && ((g_prof.mask >> c) & 1) && (a = g_prof.get())) (void)hipEventRecord(a, st);
+}
+tx::ProfScope::~ProfScope() {
+  if (!a) return;
+  hipEvent_t b = g_prof.get();
+  if (!b) return;
+  (void)hipEventRecord(b, st);
+  g_prof.recs.push_back({cls, a, b, fl, by});
+}
 
 extern "C" {
 

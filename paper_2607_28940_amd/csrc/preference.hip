@@ -1,0 +1,298 @@
+// Preference loss over the action head's logits: paired log ratios.
+//
+// For row r with logits z and observed action c: log p_r = z_c - lse, lse = log
+// sum_j exp z_j. An answer's log p is the sum over its rows; a pair's margin is
+// m = beta ((log p_w - ref_w) - (log p_l - ref_l)) and its loss
+//   -(1 - eps) log sigmoid(m) - eps log sigmoid(-m),
+// whose derivative by m is sigmoid(m) - (1 - eps). So a row's gradient is
+//   dz = coef (onehot_c - softmax z),  coef = +- dloss beta (sigmoid(m) - (1 - eps)).
+// The margin needs every row of both answers before any gradient exists, so the
+// logits are read twice: once for lse (kept per row) and log p, once for dz.
+// Both passes are bound by that traffic.
+#include "preference.h"
+#include "wave_reduce.h"
+
+namespace tx {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float to_f(bf16 x) { return (float)x; }
+__device__ __forceinline__ float to_f(float x) { return x; }
+
+// (max, sum of exp(x - max)) of two disjoint sets; empty: (-inf, 0).
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2);
+  const float ref = top == -INFINITY ? 0.f : top;
+  s = s * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * kLog2e);
+  m = top;
+}
+
+// 16 bytes of a row as floats
+template <class T>
+struct Vec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  T x[N];
+};
+template <class T>
+__device__ __forceinline__ Vec<T> load_vec(const T* p) {
+  return __builtin_bit_cast(Vec<T>, *reinterpret_cast<const u32x4_t*>(p));
+}
+
+// Elements of a row before its first 16-byte boundary.
+template <class T>
+__device__ __forceinline__ int head_of(const T* row, int k) {
+  return min(k, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));
+}
+
+__device__ __forceinline__ void finish_row(float m, float s, float z_act, bool counts, float* lse, float* picked) {
+  const float l = m == -INFINITY ? -INFINITY : m + logf(s);
+  *lse = l;
+  *picked = counts && l != -INFINITY ? z_act - l : 0.f;
+}
+
+// k <= 64: W lanes (a power of two >= k) hold a row, one element each.
+template <class T>
+__global__ __launch_bounds__(256) void pref_rows_narrow(const T* __restrict__ z, int64_t ld, int k, int W,
+                                                       const int32_t* __restrict__ act, int64_t row0, int64_t n,
+                                                       float* __restrict__ row_lse, float* __restrict__ picked) {
+  const int j = threadIdx.x & (W - 1);
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / W;
+  const bool ok = i < n;
+  const int a = ok ? act[row0 + i] : -1;
+  const float x = ok && j < k ? to_f(z[(row0 + i) * ld + j]) : -INFINITY;
+  float m = x;
+  for (int d = 1; d < W; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  float s = m == -INFINITY ? 0.f : expf(x - m);
+  float za = j == a ? x : 0.f;
+  for (int d = 1; d < W; d <<= 1) s += __shfl_xor(s, d), za += __shfl_xor(za, d);
+  // (a not finite logit elsewhere stays out of za; the action's own stays in)
+  if (ok && j == 0) finish_row(m, s, za, a >= 0 && a < k, row_lse + row0 + i, picked + i);
+}
+
+// The scalar head: logits [0, s], lse = log(1 + exp s), action 1 picks s.
+template <class T>
+__global__ __launch_bounds__(256) void pref_rows_scalar(const T* __restrict__ z, int64_t ld,
+                                                       const int32_t* __restrict__ act, int64_t row0, int64_t n,
+                                                       float* __restrict__ row_lse, float* __restrict__ picked) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int a = act[row0 + i];
+  const float s = to_f(z[(row0 + i) * ld]);
+  // log(1 + exp s) = max(s, 0) + log1p(exp(-|s|)); log p of the action directly,
+  // so that a sure answer keeps its digits
+  const float tail = log1pf(expf(-fabsf(s)));
+  row_lse[row0 + i] = fmaxf(s, 0.f) + tail;
+  picked[i] = a == 1 ? -(fmaxf(-s, 0.f) + tail) : a == 0 ? -(fmaxf(s, 0.f) + tail) : 0.f;
+}
+
+// Wider rows: a block of 256 per row, 16 bytes a lane between the row's ragged
+// ends, each thread its own running maximum and sum.
+template <class T>
+__global__ __launch_bounds__(256) void pref_rows_wide(const T* __restrict__ z, int64_t ld, int k,
+                                                     const int32_t* __restrict__ act, int64_t row0,
+                                                     float* __restrict__ row_lse, float* __restrict__ picked) {
+  __shared__ float sm[4], ss[4];
+  constexpr int N = Vec<T>::N;
+  const int tid = threadIdx.x;
+  const int64_t i = blockIdx.x, row = row0 + i;
+  const T* const p = z + row * ld;
+  const int head = head_of(p, k), nv = (k - head) / N, tail = head + nv * N;
+  float m = -INFINITY, s = 0.f;
+  auto take = [&](const Vec<T>& v) {
+    float x[N], top = m;
+#pragma unroll
+    for (int t = 0; t < N; ++t) x[t] = to_f(v.x[t]), top = fmaxf(top, x[t]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    s *= __builtin_amdgcn_exp2f((m - ref) * kLog2e);
+#pragma unroll
+    for (int t = 0; t < N; ++t) s += __builtin_amdgcn_exp2f((x[t] - ref) * kLog2e);
+    m = top;
+  };
+  for (int e = tid; e < head; e += 256) join(m, s, to_f(p[e]), 1.f);
+  for (int e = tail + tid; e < k; e += 256) join(m, s, to_f(p[e]), 1.f);
+  const T* const q = p + head;
+  int v = tid;
+  for (; v + 768 < nv; v += 1024) {
+    const Vec<T> a0 = load_vec(q + (int64_t)v * N), a1 = load_vec(q + (int64_t)(v + 256) * N),
+                 a2 = load_vec(q + (int64_t)(v + 512) * N), a3 = load_vec(q + (int64_t)(v + 768) * N);
+    take(a0), take(a1), take(a2), take(a3);
+  }
+  for (; v < nv; v += 256) take(load_vec(q + (int64_t)v * N));
+  const float top = wave_max(m);
+  const float ref = top == -INFINITY ? 0.f : top;
+  s = wave_sum(s * __builtin_amdgcn_exp2f((m - ref) * kLog2e));
+  if ((tid & 63) == 0) sm[tid >> 6] = top, ss[tid >> 6] = s;
+  __syncthreads();
+  if (tid == 0) {
+    m = sm[0], s = ss[0];
+    for (int w = 1; w < 4; ++w) join(m, s, sm[w], ss[w]);
+    const int a = act[row];
+    const bool counts = a >= 0 && a < k;
+    finish_row(m, s, counts ? to_f(p[a]) : 0.f, counts, row_lse + row, picked + i);
+  }
+}
+
+__device__ __forceinline__ double wave_sum_f64(double x) {
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+__device__ __forceinline__ double margin_of(const float* logp2, const float* ref, int pair, float beta) {
+  const double rw = ref ? (double)ref[2 * pair] : 0.0, rl = ref ? (double)ref[2 * pair + 1] : 0.0;
+  return (double)beta * (((double)logp2[0] - rw) - ((double)logp2[1] - rl));
+}
+
+// A block of two waves per pair, a wave per answer. An answer may have a
+// thousand rows of a few nats each, of which the margin keeps a difference: the
+// sum is held in 64 bits.
+__global__ __launch_bounds__(128) void pref_pairs_kernel(const float* __restrict__ picked,
+                                                        const int32_t* __restrict__ offs, const float* ref, float beta,
+                                                        float eps, float* __restrict__ logp, float* __restrict__ loss) {
+  __shared__ float both[2];
+  const int pair = blockIdx.x, w = threadIdx.x >> 6, lane = threadIdx.x & 63, ans = 2 * pair + w;
+  double x = 0.0;
+  for (int r = offs[ans] + lane; r < offs[ans + 1]; r += 64) x += (double)picked[r];
+  x = wave_sum_f64(x);
+  if (lane == 0) logp[ans] = both[w] = (float)x;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const double m = margin_of(both, ref, pair, beta);
+    const double tail = log1p(exp(-fabs(m)));
+    loss[pair] = (float)((1.0 - (double)eps) * (fmax(-m, 0.0) + tail) + (double)eps * (fmax(m, 0.0) + tail));
+  }
+}
+
+__global__ __launch_bounds__(128) void pref_coef_kernel(const int32_t* __restrict__ offs, const float* ref,
+                                                       const float* __restrict__ logp, const float* dloss, float beta,
+                                                       float eps, float* __restrict__ coef) {
+  const int pair = blockIdx.x, w = threadIdx.x >> 6, lane = threadIdx.x & 63, ans = 2 * pair + w;
+  const double m = margin_of(logp + 2 * pair, ref, pair, beta);
+  const double slope = eps * (1.0 / (1.0 + exp(-m))) - (1.0 - (double)eps) * (1.0 / (1.0 + exp(m)));
+  const float c = (float)((w ? -slope : slope) * (double)beta * (double)dloss[pair]);
+  for (int r = offs[ans] + lane; r < offs[ans + 1]; r += 64) coef[r] = c;
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void pref_grad_narrow(const T* __restrict__ z, int64_t ld, int k, int W,
+                                                       const int32_t* __restrict__ act, int64_t row0, int64_t n,
+                                                       const float* __restrict__ row_lse,
+                                                       const float* __restrict__ coef, T* __restrict__ dz, int64_t ldd) {
+  const int j = threadIdx.x & (W - 1);
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / W;
+  if (i >= n || j >= k) return;
+  const int a = act[row0 + i];
+  const float l = row_lse[row0 + i];
+  float g = 0.f;
+  if (a >= 0 && a < k && l != -INFINITY) g = coef[i] * ((j == a ? 1.f : 0.f) - expf(to_f(z[(row0 + i) * ld + j]) - l));
+  dz[(row0 + i) * ldd + j] = (T)g;
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void pref_grad_scalar(const T* __restrict__ z, int64_t ld,
+                                                       const int32_t* __restrict__ act, int64_t row0, int64_t n,
+                                                       const float* __restrict__ coef, T* __restrict__ dz, int64_t ldd) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int a = act[row0 + i];
+  const float s = to_f(z[(row0 + i) * ld]);
+  // 1 - sigmoid(s) = sigmoid(-s): no difference of near equals
+  float g = 0.f;
+  if (a == 1) g = coef[i] * (1.f / (1.f + expf(s)));
+  else if (a == 0) g = -coef[i] * (1.f / (1.f + expf(-s)));
+  dz[(row0 + i) * ldd] = (T)g;
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void pref_grad_wide(const T* __restrict__ z, int64_t ld, int k,
+                                                     const int32_t* __restrict__ act, int64_t row0,
+                                                     const float* __restrict__ row_lse, const float* __restrict__ coef,
+                                                     T* __restrict__ dz, int64_t ldd) {
+  constexpr int N = Vec<T>::N;
+  const int tid = threadIdx.x;
+  const int64_t i = blockIdx.x, row = row0 + i;
+  const T* const p = z + row * ld;
+  T* const o = dz + row * ldd;
+  const int a = act[row];
+  const float l = row_lse[row];
+  const bool counts = a >= 0 && a < k && l != -INFINITY;
+  const float c = counts ? coef[i] : 0.f, ref = counts ? l : 0.f;
+  auto grad = [&](float x, int e) {
+    const float soft = __builtin_amdgcn_exp2f((x - ref) * kLog2e);
+    return counts ? c * ((e == a ? 1.f : 0.f) - soft) : 0.f;
+  };
+  // 16-byte pieces where logits and gradients are aligned alike
+  const bool alike = (((uintptr_t)p ^ (uintptr_t)o) & 15) == 0;
+  const int head = alike ? head_of(p, k) : k, nv = (k - head) / N, tail = head + nv * N;
+  for (int e = tid; e < head; e += 256) o[e] = (T)grad(to_f(p[e]), e);
+  for (int e = tail + tid; e < k; e += 256) o[e] = (T)grad(to_f(p[e]), e);
+#pragma unroll 4
+  for (int v = tid; v < nv; v += 256) {
+    const int e = head + v * N;
+    const Vec<T> x = load_vec(p + e);
+    Vec<T> y;
+#pragma unroll
+    for (int t = 0; t < N; ++t) y.x[t] = (T)grad(to_f(x.x[t]), e + t);
+    *reinterpret_cast<u32x4_t*>(o + e) = __builtin_bit_cast(u32x4_t, y);
+  }
+}
+
+int lanes_for(int k) {
+  int w = 2;
+  while (w < k) w <<= 1;
+  return w;
+}
+
+template <class T>
+hipError_t rows(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0, int64_t n, float* lse, float* picked,
+                hipStream_t s) {
+  if (k == 1) {
+    pref_rows_scalar<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(z, ld, act, row0, n, lse, picked);
+  } else if (k <= 64) {
+    const int W = lanes_for(k), per = 256 / W;
+    pref_rows_narrow<T><<<(unsigned)((n + per - 1) / per), 256, 0, s>>>(z, ld, k, W, act, row0, n, lse, picked);
+  } else {
+    pref_rows_wide<T><<<(unsigned)n, 256, 0, s>>>(z, ld, k, act, row0, lse, picked);
+  }
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t grad(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0, int64_t n, const float* lse,
+                const float* coef, T* dz, int64_t ldd, hipStream_t s) {
+  if (k == 1) {
+    pref_grad_scalar<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(z, ld, act, row0, n, coef, dz, ldd);
+  } else if (k <= 64) {
+    const int W = lanes_for(k), per = 256 / W;
+    pref_grad_narrow<T><<<(unsigned)((n + per - 1) / per), 256, 0, s>>>(z, ld, k, W, act, row0, n, lse, coef, dz, ldd);
+  } else {
+    pref_grad_wide<T><<<(unsigned)n, 256, 0, s>>>(z, ld, k, act, row0, lse, coef, dz, ldd);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pref_rows(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
+                            int64_t n, float* row_lse, float* picked, hipStream_t s) {
+  return bf ? rows((const bf16*)logits, ld, k, act, row0, n, row_lse, picked, s)
+            : rows((const float*)logits, ld, k, act, row0, n, row_lse, picked, s);
+}
+hipError_t launch_pref_pairs(const float* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
+                             float eps, float* logp, float* loss, hipStream_t s) {
+  pref_pairs_kernel<<<n_pairs, 128, 0, s>>>(picked, offs, ref, beta, eps, logp, loss);
+  return hipGetLastError();
+}
+hipError_t launch_pref_coef(const int32_t* offs, int32_t n_pairs, const float* ref, const float* logp,
+                            const float* dloss, float beta, float eps, float* coef, hipStream_t s) {
+  pref_coef_kernel<<<n_pairs, 128, 0, s>>>(offs, ref, logp, dloss, beta, eps, coef);
+  return hipGetLastError();
+}
+hipError_t launch_pref_grad(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
+                            int64_t n, const float* row_lse, const float* coef, void* dlogits, int64_t ldd,
+                            hipStream_t s) {
+  return bf ? grad((const bf16*)logits, ld, k, act, row0, n, row_lse, coef, (bf16*)dlogits, ldd, s)
+            : grad((const float*)logits, ld, k, act, row0, n, row_lse, coef, (float*)dlogits, ldd, s);
+}
+
+}  // namespace tx

@@ -1,0 +1,380 @@
+// Shared pieces of the training attention kernels (train_fwd.hip, train_dq.hip,
+// train_dkv.hip): records the host hands them, LDS tile layout, fragment reads
+// and products, for bf16 and fp32 tensors of packed rows.
+//
+// Mathematics. For query row i and key row j of one group (a history, or a
+// user's events and history)
+//   t_ij = scale q_i.k_j + bias(i, j),  P = softmax over the visible j,
+//   O_i = sum_j P_ij v_j,  lse_i = log sum_j exp(t_ij)
+// and, given dO,
+//   D_i = dO_i.O_i,  dS_ij = P_ij (dO_i.v_j - D_i),
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,
+//   dv_j = sum_i P_ij dO_i,  dbias_b = sum over pairs of bucket b of dS_ij.
+// P is recomputed from lse, so nothing of the size of t is kept. Logits live in
+// the base-2 domain (scaled by log2 e, exponentiated with exp2), fp32.
+#pragma once
+
+#include "tx_internal.h"
+#include "wave_reduce.h"
+
+namespace tx {
+
+// A group of a call, rows counted from the start of the tensors. Units are the
+// blocks of work of a launch per head: for query-side launches (forward, dq)
+// the group owns units unit_q .. , parts_q per block of kTrainRows queries, for
+// the key-side launch (dk, dv) unit_k .. , parts_k per block of kTrainRows
+// keys. Groups whose blocks are divided (parts > 1) keep their partial results
+// in slots from slot_q / slot_k on. qt0: its first entry in the 64-row query
+// tile list; e0 .. e1 - 1: its events.
+struct TrainGroup {
+  int32_t q0, nq, k0, nk;
+  int32_t unit_q, parts_q, slot_q, qt0;
+  int32_t unit_k, parts_k, slot_k, e0;
+  int32_t e1, pad[3];
+};
+constexpr int kTrainRows = 128;   // queries (forward, dq) or keys (dk, dv) of a block: 4 waves of 32
+constexpr int kTrainQTile = 64;   // granularity of the per-tile key limits
+constexpr int kTrainMaxRel = 2048;
+
+struct TileLim {
+  int32_t lo, hi;  // smallest and largest number of visible keys among a tile's rows
+};
+
+// Rows of a tensor: element (row, head, f) at p + row * row + head * head
+// bytes + f elements.
+struct HeadRows {
+  char* p;
+  int64_t row, head;
+};
+
+struct TrainArgs {
+  const TrainGroup* groups;
+  int32_t n_groups, n_units, H, G;  // H query heads, G key heads
+  HeadRows q, k, v, o, dO, dq, dk, dv;
+  float* lse;           // [H][lse_ld], natural logarithm
+  int64_t lse_ld;
+  float* D;             // [H][D_ld], from row q_base on
+  int64_t D_ld;
+  const void* rel;      // [H][R] in the tensors' type
+  int32_t R;
+  const int32_t* row_lim;   // event form: visible keys of each query row (from row q_base on)
+  const TileLim* tile_lim;
+  int32_t q_base;
+  float scale, scale_log2;
+  float* partial;       // slots of divided blocks
+  float* drel_part;     // [unit][H][R] sums of dS by bucket
+};
+
+hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_fwd_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_dq_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
+hipError_t launch_train_dkv_merge(bool bf, int dh, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
+// drel[h][b] from the units' sums; scratch: [chunks][H][R] floats, chunks = ceil(units / 64)
+hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s);
+// row_lim and tile_lim of the event form from the events' row offsets and prefixes
+hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
+                               const int32_t* ev_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
+                               hipStream_t s);
+
+// floats of one partial slot
+inline size_t train_fwd_slot(int dh) { return (size_t)kTrainRows * (dh + 2); }
+inline size_t train_dq_slot(int dh) { return (size_t)kTrainRows * dh; }
+inline size_t train_dkv_slot(int dh) { return (size_t)2 * kTrainRows * dh; }
+
+#ifdef __HIPCC__
+
+constexpr float kTrainLog2e = 1.4426950408889634f, kTrainLn2 = 0.6931471805599453f;
+constexpr float kBiasMasks = -1e30f;  // a bias at or below it masks (the lowest values of bf16 and fp32 do)
+// Entries of the padded bias table on either side of the buckets: distances
+// from -kBiasPad (not visible) to R - 1 + kBiasPad (last bucket) of a tile that
+// touches the buckets.
+constexpr int kBiasPad = 96;
+__host__ __device__ inline int bias_entries(int R) { return R + 2 * kBiasPad; }
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
+typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) floatx4 lds_floatx4;
+typedef __attribute__((address_space(3))) int lds_int;
+
+// The group of unit u: the last one whose first unit is <= u (64-ary search by
+// the lanes of a wave; uniform).
+template <bool KEY_SIDE>
+__device__ __forceinline__ int find_group(const TrainGroup* __restrict__ g, int n, int u, int lane) {
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lane * step;
+    bool ok = false;
+    if (i < n) ok = (KEY_SIDE ? g[lo + i].unit_k : g[lo + i].unit_q) <= u;
+    const int c = max(1, (int)__popcll(__ballot(ok)));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Geometry of a tile of rows of DH elements in LDS. 16-byte unit u of row r
+// sits at u ^ swz(r). swz is linear over the bits of r, is different for 16
+// neighbouring rows (row-wise fragment reads: 16 lanes per pass read the same
+// unit of 16 rows) and moves 4 neighbouring rows to different groups of 4
+// units (the transposing reads of bf16 tiles take 4 units of 4 rows at a time),
+// so both reads spread over the 64 banks.
+template <class T, int DH>
+struct Geo {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int RB = DH * (int)sizeof(T);  // bytes of a row
+  static constexpr int UPR = RB / 16;
+  static constexpr int NC = RB / 32;              // 32-byte chunks: two lanes' fragments each
+  static constexpr int NB = DH / 32;              // 32-feature blocks of an accumulator
+  static __host__ __device__ constexpr int swz(int r) {
+    return BF ? (UPR == 16  ? ((r & 3) << 2) | ((r >> 2) & 3)
+                 : UPR == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3)
+                            : (r >> 2) & 3)
+              : (UPR >= 16 ? ((r & 4) << 1) | ((r & 8) >> 1) | (r & 3) : (r >> 1) & 7);
+  }
+};
+
+// Fragment reads and products of one wave.
+//   row fragment c of row r: the lane's 16 bytes (lanes 0-31 the first half of
+//   chunk c of rows 0 .. 31, lanes 32-63 the second half)
+//   rows_mma: acc[m][n] += sum_f A[m][f] B[n][f] from row fragments
+//   cols_mma: acc[f][n] += sum_r tile[r][f] X[r][n], X in the accumulator
+//   layout (lane: column n = lane % 32, register v: row 8 (v / 4) + 4 (lane /
+//   32) + v % 4), which is the layout in which X was computed
+template <class T, int DH>
+struct Wave {
+  using G = Geo<T, DH>;
+  static constexpr bool BF = G::BF;
+  int row_off, col_off;  // lane parts of the LDS byte offsets
+  __device__ __forceinline__ explicit Wave(int lane) {
+    const int l32 = lane & 31, hi = lane >> 5;
+    row_off = l32 * G::RB + ((hi ^ G::swz(l32)) << 4);
+    if (BF) {
+      const int i = lane & 15, half = (lane >> 4) & 1, r = 4 * hi + (i >> 2);
+      col_off = r * G::RB + (((2 * half + ((i & 3) >> 1)) ^ G::swz(r)) << 4) + ((i & 1) << 3);
+    } else {
+      col_off = 4 * hi * G::RB + (((l32 >> 2) ^ G::swz(4 * hi)) << 4) + ((l32 & 3) << 2);
+    }
+  }
+  __device__ __forceinline__ u32x4_t row_frag(const lds_char* tile, int rb, int c) const {
+    return *reinterpret_cast<const lds_u32x4*>(tile + (row_off ^ (c << 5)) + rb * 32 * G::RB);
+  }
+  static __device__ __forceinline__ floatx16 rows_mma(u32x4_t a, u32x4_t b, floatx16 c) {
+    if constexpr (BF) {
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                     0, 0);
+    } else {
+      const floatx4 x = __builtin_bit_cast(floatx4, a), y = __builtin_bit_cast(floatx4, b);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[t], y[t], c, 0, 0, 0);
+      return c;
+    }
+  }
+  // bf16: 8 rows of column 32 db + lane % 32, rows 32 rb + 16 h + 8 (t / 4) + 4 (lane / 32) + t % 4
+  __device__ __forceinline__ bf16x8 col_frag(const lds_char* tile, int rb, int h, int db) const {
+    const lds_char* p = tile + (32 * rb + 16 * h) * G::RB;
+    const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (col_off ^ (db << 6))));
+    const s16x4_t b =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * G::RB + (col_off ^ ((db << 6) | (G::swz(8) << 4)))));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // fp32: row 32 rb + 8 (v / 4) + 4 (lane / 32) + v % 4 of column 32 db + lane % 32
+  __device__ __forceinline__ float col_elem(const lds_char* tile, int rb, int v, int db) const {
+    const int rc = 8 * (v >> 2) + (v & 3);
+    return *reinterpret_cast<const lds_float*>(tile + (32 * rb + rc) * G::RB +
+                                               (col_off ^ (((8 * db) ^ G::swz(rc)) << 4)));
+  }
+  static __device__ __forceinline__ bf16x8 pack(const floatx16& x, int h) {
+    bf16x8 p;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) p[t] = (bf16)x[8 * h + t];
+    return p;
+  }
+  __device__ __forceinline__ void cols_mma(const lds_char* tile, int rb, const floatx16& x,
+                                           floatx16 (&acc)[G::NB]) const {
+    if constexpr (BF) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 p = pack(x, h);
+#pragma unroll
+        for (int db = 0; db < G::NB; ++db)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(tile, rb, h, db), p, acc[db], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+#pragma unroll
+        for (int db = 0; db < G::NB; ++db)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(col_elem(tile, rb, v, db), x[v], acc[db], 0, 0, 0);
+    }
+  }
+  // Whether the 32 rows hold an infinity or a NaN (uniform).
+  __device__ __forceinline__ bool rows_not_finite(const lds_char* tile, int rb) const {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int c = 0; c < G::NC; ++c) {
+      const u32x4_t w = row_frag(tile, rb, c);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        bad |= BF ? ((w[t] & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((w[t] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+    }
+    return __any(bad != 0);
+  }
+  // cols_mma for rows that hold infinities or NaN and an X whose bit v of
+  // `vis` tells whether X's register v belongs to a visible pair: a masked pair
+  // adds nothing (0 x NaN would), a visible one makes the sum NaN. The finite
+  // values go through the same product in the same order, and a second product
+  // of indicators finds the sums that a value not finite reaches, so the other
+  // sums keep their bits. Rare.
+  __device__ __forceinline__ void cols_mma_strict(const lds_char* tile, int rb, const floatx16& x, uint32_t vis,
+                                                  floatx16 (&acc)[G::NB]) const {
+#pragma unroll
+    for (int db = 0; db < G::NB; ++db) {
+      floatx16 hit;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) hit[v] = 0.f;
+      if constexpr (BF) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 a = col_frag(tile, rb, h, db), bad, seen;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const bool fin = __builtin_isfinite((float)a[t]);
+            bad[t] = fin ? (bf16)0.f : (bf16)1.f;
+            a[t] = fin ? a[t] : (bf16)0.f;
+            seen[t] = (vis >> (8 * h + t)) & 1 ? (bf16)1.f : (bf16)0.f;
+          }
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pack(x, h), acc[db], 0, 0, 0);
+          hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, seen, hit, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float a = col_elem(tile, rb, v, db);
+          const bool fin = __builtin_isfinite(a);
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(fin ? a : 0.f, x[v], acc[db], 0, 0, 0);
+          hit = __builtin_amdgcn_mfma_f32_32x32x2f32(fin ? 0.f : 1.f, (vis >> v) & 1 ? 1.f : 0.f, hit, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] = hit[v] > 0.f ? __builtin_nanf("") : acc[db][v];
+    }
+  }
+};
+
+// Copies of ROWS rows of DH elements from a tensor into an LDS tile, straight
+// from HBM/L2 (no registers), by the four waves of a block: piece p (1 KB of
+// the tile) goes to wave p % 4. Rows past `rows` read as zeros (they lie beyond
+// the buffer resource's extent). The swizzle is applied on the global side.
+template <class T, int DH, int ROWS>
+struct TileDma {
+  using G = Geo<T, DH>;
+  static constexpr int PER = ROWS * G::RB / 4096;  // pieces of a wave
+  uint32_t off[PER];
+  int wave;
+  uint32_t ldb;
+  __device__ __forceinline__ TileDma(int wave_, int lane, int64_t row_bytes) : wave(wave_), ldb((uint32_t)row_bytes) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int r = (wave + 4 * u) * (1024 / G::RB) + lane / G::UPR, s = lane % G::UPR;
+      off[u] = (uint32_t)r * ldb + ((uint32_t)(s ^ G::swz(r)) << 4);
+    }
+  }
+  // rows: rows left in the tensor's group from `first` on (>= 1)
+  __device__ __forceinline__ void load(const char* first, int rows, lds_char* tile) const {
+    const int n = min(rows, ROWS);
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)((uint32_t)(n - 1) * ldb + G::RB), 0x00020000);
+#pragma unroll
+    for (int u = 0; u < PER; ++u)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + (wave + 4 * u) * 1024), 16, (int)off[u], 0, 0, 0);
+  }
+};
+
+// The lane's fragments of one row (lane % 32) straight from memory; zeros
+// where the row does not exist.
+template <class T, int DH>
+__device__ __forceinline__ void load_row_frags(const char* row, bool exists, int hi, u32x4_t (&f)[Geo<T, DH>::NC]) {
+#pragma unroll
+  for (int c = 0; c < Geo<T, DH>::NC; ++c) f[c] = u32x4_t{0, 0, 0, 0};
+  if (exists) {
+#pragma unroll
+    for (int c = 0; c < Geo<T, DH>::NC; ++c) f[c] = *reinterpret_cast<const u32x4_t*>(row + 32 * c + 16 * hi);
+  }
+}
+
+// Parks a wave's accumulator (columns = rows of the output, 32 of them) in LDS
+// as output rows in T and stores them row-contiguously, 16 bytes a lane. stage:
+// 32 * RB bytes of this wave's own. mul: factor of the lane's column.
+template <class T, int DH>
+__device__ __forceinline__ void store_rows(const floatx16 (&acc)[Geo<T, DH>::NB], float mul, lds_char* stage, char* out,
+                                           int64_t row_bytes, int n_rows, int lane) {
+  using G = Geo<T, DH>;
+  const int l32 = lane & 31, hi = lane >> 5;
+#pragma unroll
+  for (int db = 0; db < G::NB; ++db)
+#pragma unroll
+    for (int gq = 0; gq < 4; ++gq) {
+      if constexpr (G::BF) {
+        bf16x4 w;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = (bf16)(acc[db][4 * gq + t] * mul);
+        *reinterpret_cast<lds_u32x2*>(stage + l32 * G::RB + (((4 * db + gq) ^ G::swz(l32)) << 4) + 8 * hi) =
+            __builtin_bit_cast(u32x2_t, w);
+      } else {
+        floatx4 w;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = acc[db][4 * gq + t] * mul;
+        *reinterpret_cast<lds_u32x4*>(stage + l32 * G::RB + (((8 * db + 2 * gq + hi) ^ G::swz(l32)) << 4)) =
+            __builtin_bit_cast(u32x4_t, w);
+      }
+    }
+  __builtin_amdgcn_wave_barrier();
+  constexpr int RPI = 64 / G::UPR;
+#pragma unroll
+  for (int k = 0; k < 32 / RPI; ++k) {
+    const int r = k * RPI + lane / G::UPR, u = lane % G::UPR;
+    const u32x4_t w = *reinterpret_cast<const lds_u32x4*>(stage + r * G::RB + ((u ^ G::swz(r)) << 4));
+    if (r < n_rows) *reinterpret_cast<u32x4_t*>(out + r * row_bytes + 16 * u) = w;
+  }
+}
+
+// The accumulator as fp32 rows of a partial slot (row = the lane's column).
+template <class T, int DH>
+__device__ __forceinline__ void store_partial(const floatx16 (&acc)[Geo<T, DH>::NB], float* row, int hi) {
+#pragma unroll
+  for (int db = 0; db < DH / 32; ++db)
+#pragma unroll
+    for (int gq = 0; gq < 4; ++gq) {
+      floatx4 w;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = acc[db][4 * gq + t];
+      *reinterpret_cast<floatx4*>(row + 32 * db + 8 * gq + 4 * hi) = w;
+    }
+}
+
+// The head's bias in base-2 units, padded: entry kBiasPad + d is the bias of
+// distance d, minus infinity for d < 0. R = 0: no bias.
+template <class T>
+__device__ __forceinline__ float bias_value(const T* __restrict__ rel, int R, int h, int d) {
+  if (d < 0) return -INFINITY;
+  if (R == 0) return 0.f;
+  const float b = (float)rel[(size_t)h * R + min(d, R - 1)];
+  return b <= kBiasMasks ? -INFINITY : b * kTrainLog2e;
+}
+template <class T>
+__device__ __forceinline__ void stage_bias(lds_float* tab, const T* __restrict__ rel, int R, int h, int tid) {
+  for (int i = tid; i < bias_entries(R); i += 256) tab[i] = bias_value(rel, R, h, i - kBiasPad);
+}
+
+#endif  // __HIPCC__
+
+}  // namespace tx

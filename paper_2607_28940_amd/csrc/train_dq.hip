@@ -1,0 +1,312 @@
+// Backward of the training attention (train_attn.h), query side: dq of 128
+// queries of one (group, head) per block, the bias gradient's sums over those
+// queries, and D (read again by the key side).
+//
+// The gradients of keys and values are summed over queries and those of
+// queries over keys, so one of the two would need atomic adds across blocks if
+// a single kernel made both; two kernels that each recompute S and dP (seven
+// tile products in all instead of five) keep every sum in one block in a fixed
+// order.
+#include "train_attn.h"
+
+namespace tx {
+namespace {
+
+template <class T>
+constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
+
+template <class T, int DH>
+constexpr int dq_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
+
+// Per wave and 32 keys: S^T = K Q^T, dP^T = V dO^T (lanes = queries, so lse and
+// D are one register each), dS = P (dP - D), dQ^T += K^T dS^T with dS^T taken
+// from the accumulators. dS is rounded to bf16 for that product (relative 2^-9
+// of each term, as P in the forward).
+//
+// Bias gradient: only tiles that touch the buckets below the last one add their
+// dS, per distance, to a padded table in LDS, one per wave and half wave, so
+// that the lanes of one instruction go to different entries and each table is
+// summed in program order. The last bucket needs no sums: every row's dS adds
+// up to zero, so its gradient is minus the sum of the others.
+template <class T, int DH, bool REL>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(const TrainArgs a) {
+  using Gm = Geo<T, DH>;
+  using W = Wave<T, DH>;
+  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = dq_tile_bytes<T, DH>();
+  extern __shared__ __align__(1024) char smem_[];
+  lds_char* const smem = (lds_char*)smem_;
+  lds_float* const tab = (lds_float*)(smem + 4 * TB);
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
+  const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
+  const int local = unit - g.unit_q, part = local % parts;
+  const int qb = REL ? blocks - 1 - local / parts : local / parts;
+  const int q_first = qb * kTrainRows;
+  const int hk = h / (a.H / a.G);
+  const int R = REL ? a.R : 0, entries = bias_entries(R);
+  const bool sums = REL && R > 1;
+  lds_float* const sub = tab + entries;
+
+  int k_end;
+  if (REL) {
+    k_end = min(g.nq, q_first + kTrainRows);
+  } else {
+    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    k_end = tl[0].hi;
+    if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+  }
+  if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
+  if (sums)
+    for (int i = tid; i < 8 * entries; i += 256) sub[i] = 0.f;
+  const float far = REL ? bias_value((const T*)a.rel, R, h, max(R, 1) - 1) : 0.f;
+  int t_begin = 0;
+  if (REL && far == -INFINITY) t_begin = max(0, q_first - (R - 2)) / KT;
+  int t_end = (k_end + KT - 1) / KT;
+  if (parts > 1) {
+    const int n = max(0, t_end - t_begin);
+    t_end = t_begin + (int)((int64_t)n * (part + 1) / parts);
+    t_begin += (int)((int64_t)n * part / parts);
+  }
+
+  const int q_wave = q_first + wave * 32, q_row = q_wave + l32;
+  const bool exists = q_row < g.nq;
+  const int64_t row = g.q0 + q_row;
+  u32x4_t qf[Gm::NC], df[Gm::NC];
+  load_row_frags<T, DH>(a.dO.p + row * a.dO.row + h * a.dO.head, exists, hi, df);
+  float D = 0.f;
+  {
+    u32x4_t of[Gm::NC];
+    load_row_frags<T, DH>(a.o.p + row * a.o.row + h * a.o.head, exists, hi, of);
+#pragma unroll
+    for (int c = 0; c < Gm::NC; ++c) {
+      if constexpr (Gm::BF) {
+        const bf16x8 x = __builtin_bit_cast(bf16x8, of[c]), y = __builtin_bit_cast(bf16x8, df[c]);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) D = fmaf((float)x[t], (float)y[t], D);
+      } else {
+        const floatx4 x = __builtin_bit_cast(floatx4, of[c]), y = __builtin_bit_cast(floatx4, df[c]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) D = fmaf(x[t], y[t], D);
+      }
+    }
+    D = xor32_sum(D);
+  }
+  load_row_frags<T, DH>(a.q.p + row * a.q.row + h * a.q.head, exists, hi, qf);
+  float lse2 = INFINITY;  // a row without visible keys keeps it: its probabilities are 0
+  if (exists) {
+    const float x = a.lse[(int64_t)h * a.lse_ld + row];
+    if (x != -INFINITY) lse2 = x * kTrainLog2e;
+    if (part == 0 && hi == 0) a.D[(int64_t)h * a.D_ld + row - a.q_base] = D;
+  }
+  int lim = 0;
+  if (exists) lim = REL ? q_row + 1 : a.row_lim[row - a.q_base];
+  int lim_lo, lim_hi;
+  if (REL) {
+    lim_lo = q_wave + 1;
+    lim_hi = q_wave >= g.nq ? 0 : min(q_wave + 32, g.nq);
+  } else {
+    int lo = exists ? lim : 0x7fffffff, up = lim;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      lo = min(lo, __shfl_xor(lo, m));
+      up = max(up, __shfl_xor(up, m));
+    }
+    lim_lo = uniform(lo);
+    lim_hi = uniform(up);
+  }
+
+  floatx16 dq[Gm::NB];
+#pragma unroll
+  for (int db = 0; db < Gm::NB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
+
+  const W w(lane);
+  const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
+  const char* const kp = a.k.p + (int64_t)g.k0 * a.k.row + hk * a.k.head;
+  const char* const vp = a.v.p + (int64_t)g.k0 * a.v.row + hk * a.v.head;
+  auto fetch = [&](int t, int b) {
+    const int r = t * KT;
+    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
+    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
+  };
+  if (t_begin < t_end) fetch(t_begin, 0);
+  __syncthreads();
+  for (int t = t_begin; t < t_end; ++t) {
+    const int b = (t - t_begin) & 1, k0 = t * KT;
+    if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+    const lds_char* const sK = smem + b * TB;
+    const lds_char* const sV = smem + (2 + b) * TB;
+    if (k0 < lim_hi) {
+      const bool near = REL && (q_wave - (k0 + KT - 1) < R - 1 || fabsf(far) >= 0x1p20f);
+      const bool masked = REL ? near : k0 + KT > lim_lo;
+      const int d0 = min(q_row - k0, R - 1 + kBiasPad - 1) - 4 * hi + kBiasPad;
+      const float off = far - lse2;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        floatx16 s, p;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f, p[v] = 0.f;
+#pragma unroll
+        for (int c = 0; c < Gm::NC; ++c) s = W::rows_mma(w.row_frag(sK, kb, c), qf[c], s);
+#pragma unroll
+        for (int c = 0; c < Gm::NC; ++c) p = W::rows_mma(w.row_frag(sV, kb, c), df[c], p);
+        if (!masked) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (p[v] - D);
+          w.cols_mma(sK, kb, s, dq);
+          continue;
+        }
+        uint32_t vis = 0;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = kb * 32 + 8 * (v >> 2) + (v & 3);
+          const float bias = REL ? tab[d0 - key] : 0.f;
+          const bool see = REL ? bias != -INFINITY : key < lim - k0 - 4 * hi;
+          vis |= see ? 1u << v : 0u;
+          // in two steps: a large bias rounds the logit as it did in the forward
+          const float lg = fmaf(s[v], a.scale_log2, bias);
+          s[v] = see ? __builtin_amdgcn_exp2f(lg - lse2) * (p[v] - D) : 0.f;
+        }
+        // (a row past the group's end has lse2 = inf, so it adds 0)
+        if (sums) {
+          lds_float* const mine = sub + (2 * wave + hi) * entries;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int key = kb * 32 + 8 * (v >> 2) + (v & 3);
+            if (exists) __builtin_amdgcn_ds_atomic_fadd_f32(mine + (d0 - key), s[v]);
+          }
+        }
+        if (w.rows_not_finite(sK, kb)) w.cols_mma_strict(sK, kb, s, vis, dq);
+        else w.cols_mma(sK, kb, s, dq);
+      }
+    }
+    __syncthreads();
+  }
+  if (sums) {
+    // (the loop, also an empty one, ended on a barrier)
+    float* const out = a.drel_part + ((size_t)unit * a.H + h) * R;
+    for (int d = tid; d < R; d += 256) {
+      float x = 0.f;
+      if (d < R - 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += sub[i * entries + kBiasPad + d];
+      out[d] = x;
+    }
+  }
+  if (parts > 1) {
+    float* const slot = a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) * (kTrainRows * DH);
+    store_partial<T, DH>(dq, slot + (size_t)(wave * 32 + l32) * DH, hi);
+    return;
+  }
+  if (q_wave < g.nq)
+    store_rows<T, DH>(dq, a.scale, smem + wave * 32 * Gm::RB,
+                      a.dq.p + (int64_t)(g.q0 + q_wave) * a.dq.row + h * a.dq.head, a.dq.row, g.nq - q_wave, lane);
+}
+
+template <class T, int DH>
+__global__ __launch_bounds__(256) void train_dq_merge_kernel(const TrainArgs a) {
+  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H, tid = threadIdx.x;
+  const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
+  const int parts = g.parts_q, local = unit - g.unit_q;
+  if (parts == 1 || local % parts) return;
+  const int qb = local / parts, rows = min(kTrainRows, g.nq - qb * kTrainRows);
+  constexpr size_t SLOT = (size_t)kTrainRows * DH;
+  const float* const p0 = a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * SLOT;
+  constexpr int LPR = DH / 4;
+  for (int i = tid; i < rows * LPR; i += 256) {
+    const int r = i / LPR, f = i % LPR * 4;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) {
+      const floatx4 x = *reinterpret_cast<const floatx4*>(p0 + p * SLOT * a.H + (size_t)r * DH + f);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[t] += x[t];
+    }
+    T* const out = (T*)(a.dq.p + (int64_t)(g.q0 + qb * kTrainRows + r) * a.dq.row + h * a.dq.head) + f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * a.scale);
+  }
+}
+
+// Sums of 64 units' bucket sums (the first pass) ...
+__global__ __launch_bounds__(256) void drel_chunk_kernel(const float* __restrict__ part, int n_units, int HR,
+                                                         float* __restrict__ out) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= HR) return;
+  const int u0 = blockIdx.y * 64, u1 = min(u0 + 64, n_units);
+  float x = 0.f;
+  for (int u = u0; u < u1; ++u) x += part[(size_t)u * HR + i];
+  out[(size_t)blockIdx.y * HR + i] = x;
+}
+// ... and of all chunks, the last bucket as minus the others: a block per head.
+template <class T>
+__global__ __launch_bounds__(256) void drel_head_kernel(const float* __restrict__ part, int n, int H, int R,
+                                                        T* __restrict__ drel) {
+  __shared__ float wsum[4];
+  const int h = blockIdx.x, tid = threadIdx.x;
+  float others = 0.f;
+  for (int b = tid; b < R - 1; b += 256) {
+    float x = 0.f;
+    for (int c = 0; c < n; ++c) x += part[((size_t)c * H + h) * R + b];
+    drel[(size_t)h * R + b] = (T)x;
+    others += x;
+  }
+  others = wave_sum(others);
+  if ((tid & 63) == 0) wsum[tid >> 6] = others;
+  __syncthreads();
+  if (tid == 0) drel[(size_t)h * R + R - 1] = (T)(0.f - (wsum[0] + wsum[1] + wsum[2] + wsum[3]));
+}
+
+template <class T, int DH, bool REL>
+hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
+  const size_t lds = 4 * dq_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 9 : 1) : 0);
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)train_dq_kernel<T, DH, REL>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  train_dq_kernel<T, DH, REL><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  return hipGetLastError();
+}
+template <class T, int DH>
+hipError_t dq_merge(const TrainArgs& a, hipStream_t s) {
+  train_dq_merge_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
+#define TX_CASE(T, D) return rel ? dq_launch<T, D, true>(a, s) : dq_launch<T, D, false>(a, s)
+  if (bf) {
+    if (dh == 32) TX_CASE(bf16, 32);
+    if (dh == 64) TX_CASE(bf16, 64);
+    TX_CASE(bf16, 128);
+  }
+  if (dh == 32) TX_CASE(float, 32);
+  if (dh == 64) TX_CASE(float, 64);
+  TX_CASE(float, 128);
+#undef TX_CASE
+}
+
+hipError_t launch_train_dq_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
+  if (bf) return dh == 32 ? dq_merge<bf16, 32>(a, s) : dh == 64 ? dq_merge<bf16, 64>(a, s) : dq_merge<bf16, 128>(a, s);
+  return dh == 32 ? dq_merge<float, 32>(a, s) : dh == 64 ? dq_merge<float, 64>(a, s) : dq_merge<float, 128>(a, s);
+}
+
+hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s) {
+  const int HR = a.H * a.R;
+  const float* part = a.drel_part;
+  int n = a.R > 1 ? a.n_units : 0;
+  if (n > 64) {
+    const int chunks = (n + 63) / 64;
+    drel_chunk_kernel<<<dim3((HR + 255) / 256, chunks), 256, 0, s>>>(part, n, HR, scratch);
+    part = scratch, n = chunks;
+  }
+  if (bf) drel_head_kernel<bf16><<<a.H, 256, 0, s>>>(part, n, a.H, a.R, (bf16*)drel);
+  else drel_head_kernel<float><<<a.H, 256, 0, s>>>(part, n, a.H, a.R, (float*)drel);
+  return hipGetLastError();
+}
+
+}  // namespace tx

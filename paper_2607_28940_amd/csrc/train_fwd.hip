@@ -1,0 +1,331 @@
+// Forward of the training attention (train_attn.h): O and lse of 128 queries of
+// one (group, head) per block, in one pass over the visible keys with the
+// running maximum and sum of the softmax.
+#include "train_attn.h"
+
+namespace tx {
+namespace {
+
+template <class T>
+constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
+
+template <class T, int DH>
+constexpr int fwd_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
+
+// Per wave and tile of KT keys: S^T = K Q^T with keys as rows, so a lane holds
+// KT / 2 keys of one query and the softmax needs one exchange with lane l ^ 32;
+// then O^T += V^T P^T, P^T taken from the accumulators as they are and V^T
+// fragments read from the row-major tile (bf16: transposing LDS reads).
+// K and V are double-buffered, one barrier per tile.
+template <class T, int DH, bool REL>
+__global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
+  using Gm = Geo<T, DH>;
+  using W = Wave<T, DH>;
+  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = fwd_tile_bytes<T, DH>();
+  extern __shared__ __align__(1024) char smem_[];
+  lds_char* const smem = (lds_char*)smem_;
+  lds_float* const tab = (lds_float*)(smem + 4 * TB);
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
+  const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
+  const int local = unit - g.unit_q, part = local % parts;
+  // longest blocks of a causal group first
+  const int qb = REL ? blocks - 1 - local / parts : local / parts;
+  const int q_first = qb * kTrainRows;
+  const int hk = h / (a.H / a.G);
+
+  // keys that any row of the block sees, and the block's share of them
+  int k_end;
+  if (REL) {
+    k_end = min(g.nq, q_first + kTrainRows);
+  } else {
+    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    k_end = tl[0].hi;
+    if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+  }
+  const int R = REL ? a.R : 0;
+  if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
+  const float far = REL ? bias_value((const T*)a.rel, R, h, max(R, 1) - 1) : 0.f;
+  int t_begin = 0;
+  // a last bucket that masks leaves a window of the R - 1 nearest keys
+  if (REL && far == -INFINITY) t_begin = max(0, q_first - (R - 2)) / KT;
+  int t_end = (k_end + KT - 1) / KT;
+  if (parts > 1) {
+    const int n = max(0, t_end - t_begin);
+    t_end = t_begin + (int)((int64_t)n * (part + 1) / parts);
+    t_begin += (int)((int64_t)n * part / parts);
+  }
+
+  const int q_wave = q_first + wave * 32;         // first query of the wave, within the group
+  const int q_row = q_wave + l32;
+  const bool exists = q_row < g.nq;
+  u32x4_t qf[Gm::NC];
+  load_row_frags<T, DH>(a.q.p + (int64_t)(g.q0 + q_row) * a.q.row + h * a.q.head, exists, hi, qf);
+  int lim = 0;  // visible keys of the lane's query
+  if (exists) lim = REL ? q_row + 1 : a.row_lim[g.q0 + q_row - a.q_base];
+  int lim_lo, lim_hi;  // over the wave's existing rows
+  if (REL) {
+    lim_lo = q_wave + 1;
+    lim_hi = min(q_wave + 32, g.nq);
+    if (q_wave >= g.nq) lim_hi = 0;
+  } else {
+    int lo = exists ? lim : 0x7fffffff, up = lim;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      lo = min(lo, __shfl_xor(lo, m));
+      up = max(up, __shfl_xor(up, m));
+    }
+    lim_lo = uniform(lo);
+    lim_hi = uniform(up);
+  }
+
+  floatx16 o[Gm::NB];
+#pragma unroll
+  for (int db = 0; db < Gm::NB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  const W w(lane);
+  const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
+  const char* const kp = a.k.p + (int64_t)g.k0 * a.k.row + hk * a.k.head;
+  const char* const vp = a.v.p + (int64_t)g.k0 * a.v.row + hk * a.v.head;
+  auto fetch = [&](int t, int b) {
+    const int r = t * KT;
+    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
+    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
+  };
+  if (t_begin < t_end) fetch(t_begin, 0);
+  __syncthreads();
+  for (int t = t_begin; t < t_end; ++t) {
+    const int b = (t - t_begin) & 1, k0 = t * KT;
+    if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+    const lds_char* const sK = smem + b * TB;
+    const lds_char* const sV = smem + (2 + b) * TB;
+    if (k0 < lim_hi) {
+      floatx16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+        for (int c = 0; c < Gm::NC; ++c) s[kb] = W::rows_mma(w.row_frag(sK, kb, c), qf[c], s[kb]);
+      }
+      // logits as fma(s, mul, add): plain tiles scale here, tiles that touch the
+      // buckets or the mask were brought to base-2 logits already
+      float mul = a.scale_log2, add = far;
+      const bool near = REL && (q_wave - (k0 + KT - 1) < R - 1 || fabsf(far) >= 0x1p20f);
+      const bool masked = REL ? near : k0 + KT > lim_lo;
+      // the lane's entry of the key 0 of the tile, less its 4 hi: distances beyond the
+      // padding are all in the last bucket
+      const int d0 = min(q_row - k0, R - 1 + kBiasPad - 1) - 4 * hi + kBiasPad;
+      if (masked) {
+        mul = 1.f, add = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int key = kb * 32 + 8 * (v >> 2) + (v & 3);
+            if (REL) {
+              const float bias = tab[d0 - key];
+              s[kb][v] = bias == -INFINITY ? -INFINITY : fmaf(s[kb][v], a.scale_log2, bias);
+            } else {
+              s[kb][v] = key < lim - k0 - 4 * hi ? s[kb][v] * a.scale_log2 : -INFINITY;
+            }
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+      mx = fmaf(xor32_max(mx), mul, add);
+      // The reference m moves only when this tile would push a probability
+      // above 2^8 (fine for fp32 sums and for bf16 P, whose rounding is
+      // relative); O / l does not depend on which reference was used.
+      const bool bump = mx > m + 8.f;
+      if (__any(bump)) {
+        const float m_new = bump ? mx : m;
+        const float alpha = bump ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < Gm::NB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+        m = m_new;
+      }
+      const float off = m == -INFINITY ? 0.f : add - m;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          s[kb][v] = __builtin_amdgcn_exp2f(fmaf(s[kb][v], mul, off));
+          l += s[kb][v];
+        }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        if (masked && w.rows_not_finite(sV, kb)) {
+          uint32_t vis = 0;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int key = kb * 32 + 8 * (v >> 2) + (v & 3);
+            const bool see = REL ? tab[d0 - key] != -INFINITY : key < lim - k0 - 4 * hi;
+            vis |= see ? 1u << v : 0u;
+          }
+          w.cols_mma_strict(sV, kb, s[kb], vis, o);
+        } else {
+          w.cols_mma(sV, kb, s[kb], o);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  l = xor32_sum(l);
+  if (parts > 1) {
+    float* const slot =
+        a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) * (kTrainRows * (DH + 2));
+    const int r = wave * 32 + l32;
+    store_partial<T, DH>(o, slot + (size_t)r * DH, hi);
+    if (hi == 0) {
+      slot[kTrainRows * DH + r] = m;
+      slot[kTrainRows * (DH + 1) + r] = l;
+    }
+    return;
+  }
+  // l is 0 only for a row without a visible key: its output is 0, its lse minus infinity
+  const int n_rows = g.nq - q_wave;
+  if (exists && hi == 0)
+    a.lse[(int64_t)h * a.lse_ld + g.q0 + q_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kTrainLn2;
+  if (n_rows > 0)
+    store_rows<T, DH>(o, l == 0.f ? 0.f : 1.f / l, smem + wave * 32 * Gm::RB,
+                      a.o.p + (int64_t)(g.q0 + q_wave) * a.o.row + h * a.o.head, a.o.row, n_rows, lane);
+}
+
+// Joins the parts of divided blocks: a block per (query block, head), 16 bytes of
+// output row per thread.
+template <class T, int DH>
+__global__ __launch_bounds__(256) void train_fwd_merge_kernel(const TrainArgs a) {
+  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H, tid = threadIdx.x;
+  const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
+  const int parts = g.parts_q, local = unit - g.unit_q;
+  if (parts == 1 || local % parts) return;
+  const int qb = local / parts, rows = min(kTrainRows, g.nq - qb * kTrainRows);
+  constexpr size_t SLOT = (size_t)kTrainRows * (DH + 2);
+  const float* const p0 = a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * SLOT;
+  const size_t step = SLOT * a.H;
+  constexpr int LPR = DH / 4;
+  for (int i = tid; i < rows * LPR; i += 256) {
+    const int r = i / LPR, f = i % LPR * 4;
+    float top = -INFINITY;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, p0[p * step + kTrainRows * DH + r]);
+    float l = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) {
+      const float* s = p0 + p * step;
+      const float m = s[kTrainRows * DH + r];
+      const float wgt = m == -INFINITY ? (s[kTrainRows * (DH + 1) + r] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
+      if (wgt == 0.f) continue;
+      l += wgt * s[kTrainRows * (DH + 1) + r];
+      const floatx4 x = *reinterpret_cast<const floatx4*>(s + (size_t)r * DH + f);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[t] += wgt * x[t];
+    }
+    const int64_t row = g.q0 + qb * kTrainRows + r;
+    if (f == 0) a.lse[(int64_t)h * a.lse_ld + row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kTrainLn2;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* const out = (T*)(a.o.p + row * a.o.row + h * a.o.head) + f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * inv);
+  }
+}
+
+// The event form's key limits: a wave per 64-row query tile finds each row's
+// event (the last whose first row is not past it: events may be empty) and keeps its prefix, with
+// the tile's smallest and largest.
+__global__ __launch_bounds__(64) void train_limits_kernel(const TrainGroup* __restrict__ groups, int n_groups,
+                                                         const int32_t* __restrict__ ev_row,
+                                                         const int32_t* __restrict__ ev_prefix,
+                                                         int32_t* __restrict__ row_lim, int q_base,
+                                                         TileLim* __restrict__ tile_lim) {
+  const int lane = threadIdx.x, tile = blockIdx.x;
+  // the last group whose first tile is not past this one
+  int lo = 0, n = n_groups;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lane * step;
+    const bool ok = i < n && groups[lo + i].qt0 <= tile;
+    const int c = max(1, (int)__popcll(__ballot(ok)));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  const TrainGroup g = groups[uniform(lo)];
+  const int r = (tile - g.qt0) * kTrainQTile + lane;
+  const bool exists = r < g.nq;
+  int lim = 0;
+  if (exists) {
+    const int row = g.q0 + r;
+    int a = g.e0, b = g.e1 - 1;  // last event in a .. b whose first row is <= row
+    while (a < b) {
+      const int mid = (a + b + 1) >> 1;
+      if (ev_row[mid] <= row) a = mid;
+      else b = mid - 1;
+    }
+    lim = ev_prefix[a];
+    row_lim[row - q_base] = lim;
+  }
+  int mn = exists ? lim : 0x7fffffff, mx = lim;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    mn = min(mn, __shfl_xor(mn, m));
+    mx = max(mx, __shfl_xor(mx, m));
+  }
+  if (lane == 0) tile_lim[tile] = TileLim{mn, mx};
+}
+
+template <class T, int DH, bool REL>
+hipError_t fwd(const TrainArgs& a, hipStream_t s) {
+  const size_t lds = 4 * fwd_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)train_fwd_kernel<T, DH, REL>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  train_fwd_kernel<T, DH, REL><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <class T, int DH>
+hipError_t fwd_merge(const TrainArgs& a, hipStream_t s) {
+  train_fwd_merge_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
+#define TX_CASE(T, D) return rel ? fwd<T, D, true>(a, s) : fwd<T, D, false>(a, s)
+  if (bf) {
+    if (dh == 32) TX_CASE(bf16, 32);
+    if (dh == 64) TX_CASE(bf16, 64);
+    TX_CASE(bf16, 128);
+  }
+  if (dh == 32) TX_CASE(float, 32);
+  if (dh == 64) TX_CASE(float, 64);
+  TX_CASE(float, 128);
+#undef TX_CASE
+}
+
+hipError_t launch_train_fwd_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
+  if (bf) return dh == 32 ? fwd_merge<bf16, 32>(a, s) : dh == 64 ? fwd_merge<bf16, 64>(a, s) : fwd_merge<bf16, 128>(a, s);
+  return dh == 32 ? fwd_merge<float, 32>(a, s) : dh == 64 ? fwd_merge<float, 64>(a, s) : fwd_merge<float, 128>(a, s);
+}
+
+hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
+                               const int32_t* ev_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
+                               hipStream_t s) {
+  if (n_tiles == 0) return hipSuccess;
+  train_limits_kernel<<<n_tiles, 64, 0, s>>>(groups, n_groups, ev_row, ev_prefix, row_lim, q_base, tile_lim);
+  return hipGetLastError();
+}
+
+}  // namespace tx

@@ -3,7 +3,8 @@
 Argument marshalling only: every step of the path runs in the library's HIP
 kernels. PyTorch provides device memory (weights, the page pool, workspaces,
 inputs, outputs) and the stream; the functions mirror the C ABI of
-include/transx.h (kv_cache_build, kv_cache_append, score_candidates).
+include/transx.h (kv_cache_build, kv_cache_append, score_candidates, and the
+training operators tx_rel_attn_*, tx_event_attn_*, tx_preference_*).
 If the library has not been built, loading fails loudly: there is no
 fallback implementation.
 """
@@ -49,11 +50,28 @@ class Config(ctypes.Structure):
                    int(bool(m.global_pool)), int(m.n_actions))
 
 
+class AttnConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("d_head", ctypes.c_int32), ("rel_pos_buckets", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class PreferenceConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_actions", ctypes.c_int32), ("beta", ctypes.c_float),
+                ("smoothing", ctypes.c_float)]
+
+
 _lib = None
 VP = ctypes.c_void_p
 I32P = ctypes.POINTER(ctypes.c_int32)
 I64P = ctypes.POINTER(ctypes.c_int64)
 CFGP = ctypes.POINTER(Config)
+ACFGP = ctypes.POINTER(AttnConfig)
+PCFGP = ctypes.POINTER(PreferenceConfig)
+ROWSP = ctypes.POINTER(Rows)
 
 _SIGS = {
     "tx_last_error": (ctypes.c_char_p, []),
@@ -79,6 +97,22 @@ _SIGS = {
     "score_candidates": (ctypes.c_int, [VP, ctypes.c_int32, I32P, VP, I64P, VP, I64P, VP, VP, ctypes.c_size_t, VP]),
     "score_candidates_static": (ctypes.c_int, [VP, ctypes.c_int32, I32P, VP, I64P, VP, I64P, VP, VP]),
     "score_events": (ctypes.c_int, [VP, ctypes.c_int32, I32P, I64P, VP, I64P, VP, I64P, VP, VP, ctypes.c_size_t, VP]),
+    "tx_rel_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, I64P]),
+    "tx_rel_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
+                                           ctypes.c_int64, VP, ctypes.c_size_t, VP]),
+    "tx_rel_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
+                                            ctypes.c_int64, ROWSP, ROWSP, ROWSP, ROWSP, VP, VP, ctypes.c_size_t, VP]),
+    "tx_event_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, I64P, I64P, I64P, I64P]),
+    "tx_event_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, I64P, I64P, I64P, ROWSP, ROWSP, ROWSP,
+                                             ROWSP, VP, ctypes.c_int64, VP, ctypes.c_size_t, VP]),
+    "tx_event_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, I64P, I64P, I64P, ROWSP, ROWSP, ROWSP,
+                                              ROWSP, VP, ctypes.c_int64, ROWSP, ROWSP, ROWSP, ROWSP, VP,
+                                              ctypes.c_size_t, VP]),
+    "tx_preference_workspace_bytes": (ctypes.c_size_t, [PCFGP, ctypes.c_int32, I64P]),
+    "tx_preference_forward": (ctypes.c_int, [PCFGP, ctypes.c_int32, I64P, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
+                                             ctypes.c_size_t, VP]),
+    "tx_preference_backward": (ctypes.c_int, [PCFGP, ctypes.c_int32, I64P, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
+                                              ctypes.c_int64, VP, ctypes.c_size_t, VP]),
     "tx_profile_enable": (ctypes.c_int, [ctypes.c_int32]),
     "tx_profile_select": (ctypes.c_int, [ctypes.c_uint64]),
     "tx_profile_classes": (ctypes.c_int32, []),
@@ -304,6 +338,317 @@ class KVCache:
         out = torch.empty((max(n, 0), self.model.mc.d_model), dtype=_torch_dtype(self.model.mc), device=self.device)
         check(lib().tx_kv_cache_export(self.handle, req_id, part, layer, VP(out.data_ptr()), VP(_stream(stream))))
         return out
+
+
+# ----------------------------------------------------------------- training
+# Operators of a training step. Tensors are torch tensors on one GPU, host
+# offsets anything numpy takes. A call runs on `stream` (default: the current
+# stream of the tensors' device), which has to be ordered after the work that
+# makes its inputs; outputs it allocates belong to that stream. Workspaces come
+# from torch's allocator, one per call, so calls may be captured into graphs.
+
+def _invalid(msg: str):
+    raise TxError(TX_E_INVALID, msg)
+
+
+class _On:
+    """The tensors' device and the call's stream, current for the call."""
+
+    def __init__(self, tensors: dict, stream):
+        import torch
+        dev = None
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+                _invalid(f"{name} is not a GPU tensor")
+            if dev is not None and t.device != dev:
+                _invalid(f"{name} is on {t.device}, other tensors are on {dev}")
+            dev = t.device
+        if stream is not None and stream.device != dev:
+            _invalid(f"the stream belongs to {stream.device}, the tensors are on {dev}")
+        self.dev, self.ctx = dev, None
+        if stream is not None:
+            self.ctx = torch.cuda.stream(stream)
+        elif dev.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(dev)
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        self.stream = VP(torch.cuda.current_stream().cuda_stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+    def workspace(self, nbytes: int):
+        import torch
+        # (0: the size function refused the arguments, and the call will say why)
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
+
+
+def _heads(t, name: str, dtype, shape=None) -> Rows:
+    """[rows, heads, d_head] tensor, features contiguous, as the C ABI takes it."""
+    if t.dim() != 3:
+        _invalid(f"{name} must be [rows, heads, d_head]")
+    if t.dtype != dtype:
+        _invalid(f"{name} is {t.dtype}, q is {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _invalid(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1 and t.numel():
+        _invalid(f"{name}: features of a head must be contiguous")
+    # (torch leaves the stride of a single row or head to chance)
+    head = t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return Rows(t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], head)
+
+
+def _plain(t, name: str, dtype, shape):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _invalid(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return VP(t.data_ptr() or None)
+
+
+def _dtype_of(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return TX_BF16
+    if t.dtype == torch.float32:
+        return TX_F32
+    return _invalid(f"{name} is {t.dtype}: bfloat16 or float32")
+
+
+def _attn_config(q, k, rel, scale) -> AttnConfig:
+    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
+        _invalid("q and k must be [rows, heads, d_head] of one d_head")
+    R = 0
+    if rel is not None:
+        if rel.dim() != 2 or rel.shape[0] != q.shape[1] or not rel.is_contiguous() or rel.dtype != q.dtype:
+            _invalid("rel must be a contiguous [heads, buckets] tensor of q's type")
+        R = rel.shape[1]
+    if scale is not None and not scale > 0:
+        _invalid("scale must be positive")
+    return AttnConfig(_dtype_of(q, "q"), q.shape[1], k.shape[1], q.shape[2], R, 0.0 if scale is None else float(scale))
+
+
+def _offsets(a, name: str, n: Optional[int] = None) -> np.ndarray:
+    a = _i64(a)
+    if a.ndim != 1 or len(a) < 1 or (n is not None and len(a) != n):
+        _invalid(f"{name} must be a vector of {n if n is not None else 'at least 1'} entries")
+    return a
+
+
+def _covers(rows: int, off: np.ndarray, name: str):
+    if off[-1] > rows:
+        _invalid(f"{name} offsets reach row {int(off[-1])} of {rows}")
+
+
+def _new_like(t, rows_used: bool):
+    """Output of t's shape, head by head in a row; zeros when some rows belong to no group."""
+    import torch
+    return (torch.empty if rows_used else torch.zeros)(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _new_lse(H: int, M: int, full: bool, dev):
+    import torch
+    return torch.empty((H, M), dtype=torch.float32, device=dev) if full else \
+        torch.full((H, M), -float("inf"), dtype=torch.float32, device=dev)
+
+
+def _whole(off: np.ndarray, rows: int) -> bool:
+    return off[0] == 0 and off[-1] == rows
+
+
+def rel_attention(q, k, v, rel, offsets, scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """Causal self-attention of packed sequences with the encoder's learned
+    relative position bias (tx_rel_attn_forward). q [rows, heads, d_head], k and
+    v [rows, kv heads, d_head], rel [heads, buckets] or None. Returns out like q
+    and lse fp32 [heads, rows]; rows outside the offsets keep what `out` and
+    `lse` held (0 and -inf where this call makes them)."""
+    off = _offsets(offsets, "sequence offsets")
+    with _On(dict(q=q, k=k, v=v, rel=rel, out=out, lse=lse), stream) as on:
+        cfg = _attn_config(q, k, rel, scale)
+        M, H = q.shape[0], q.shape[1]
+        kv = (M,) + tuple(k.shape[1:])
+        _covers(M, off, "sequence")
+        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype, kv), _heads(v, "v", q.dtype, kv)]
+        if out is None:
+            out = _new_like(q, _whole(off, M))
+        if lse is None:
+            lse = _new_lse(H, M, _whole(off, M), on.dev)
+        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
+        L, n, op = lib(), len(off) - 1, _p(off, I64P)
+        ws = on.workspace(L.tx_rel_attn_workspace_bytes(ctypes.byref(cfg), 0, n, op))
+        check(L.tx_rel_attn_forward(ctypes.byref(cfg), n, op, *map(ctypes.byref, a), _rel_ptr(rel), ctypes.byref(o), l,
+                                    M, VP(ws.data_ptr()), ws.numel(), on.stream))
+    return out, lse
+
+
+def rel_attention_backward(dout, q, k, v, rel, out, lse, offsets, scale: Optional[float] = None, dq=None, dk=None,
+                           dv=None, drel=None, stream=None):
+    """Gradients of rel_attention for dout, given its inputs and outputs
+    (tx_rel_attn_backward): dq, dk, dv and drel (None without a bias)."""
+    import torch
+    off = _offsets(offsets, "sequence offsets")
+    with _On(dict(q=q, k=k, v=v, rel=rel, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, drel=drel), stream) as on:
+        cfg = _attn_config(q, k, rel, scale)
+        M, H = q.shape[0], q.shape[1]
+        kv = (M,) + tuple(k.shape[1:])
+        _covers(M, off, "sequence")
+        whole = _whole(off, M)
+        dq = _new_like(q, whole) if dq is None else dq
+        dk = _new_like(k, whole) if dk is None else dk
+        dv = _new_like(v, whole) if dv is None else dv
+        if rel is not None and drel is None:
+            drel = torch.empty_like(rel)
+        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype, kv), _heads(v, "v", q.dtype, kv)]
+        g = [_heads(dout, "dout", q.dtype, q.shape), _heads(dq, "dq", q.dtype, q.shape),
+             _heads(dk, "dk", q.dtype, kv), _heads(dv, "dv", q.dtype, kv)]
+        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
+        if rel is not None:
+            _plain(drel, "drel", q.dtype, rel.shape)
+        L, n, op = lib(), len(off) - 1, _p(off, I64P)
+        ws = on.workspace(L.tx_rel_attn_workspace_bytes(ctypes.byref(cfg), 1, n, op))
+        check(L.tx_rel_attn_backward(ctypes.byref(cfg), n, op, *map(ctypes.byref, a), _rel_ptr(rel), ctypes.byref(o), l,
+                                     M, *map(ctypes.byref, g), _rel_ptr(drel if rel is not None else None),
+                                     VP(ws.data_ptr()), ws.numel(), on.stream))
+    return dq, dk, dv, (drel if rel is not None else None)
+
+
+def _f32():
+    import torch
+    return torch.float32
+
+
+def _rel_ptr(rel):
+    return VP(rel.data_ptr() or None) if rel is not None else VP()
+
+
+def _event_args(key_offsets, event_offsets, query_offsets, prefix_len):
+    ko = _offsets(key_offsets, "key offsets")
+    eo = _offsets(event_offsets, "event offsets", len(ko))
+    if eo[0] != 0 or np.any(np.diff(eo) < 0):
+        _invalid("event offsets must start at 0 and not decrease")
+    qo = _offsets(query_offsets, "query offsets", int(eo[-1]) + 1)
+    pre = _i64(prefix_len)
+    if pre.ndim != 1 or len(pre) != int(eo[-1]):
+        _invalid(f"prefix lengths must be a vector of {int(eo[-1])} entries")
+    return ko, eo, qo, pre
+
+
+def event_attention(q, k, v, key_offsets, event_offsets, query_offsets, prefix_len, scale: Optional[float] = None,
+                    out=None, lse=None, stream=None):
+    """Cross-attention of event-sliced decoding (tx_event_attn_forward): the
+    query rows of event e see the first prefix_len[e] key rows of their user. q
+    [query rows, heads, d_head], k and v [key rows, kv heads, d_head]. Returns
+    out like q and lse fp32 [heads, query rows]."""
+    where = _event_args(key_offsets, event_offsets, query_offsets, prefix_len)
+    with _On(dict(q=q, k=k, v=v, out=out, lse=lse), stream) as on:
+        cfg = _attn_config(q, k, None, scale)
+        M, H = q.shape[0], q.shape[1]
+        _covers(M, where[2], "query")
+        _covers(k.shape[0], where[0], "key")
+        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype), _heads(v, "v", q.dtype, k.shape)]
+        full = _whole(where[2], M)
+        out = _new_like(q, full) if out is None else out
+        lse = _new_lse(H, M, full, on.dev) if lse is None else lse
+        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
+        L, n, wp = lib(), len(where[0]) - 1, [_p(x, I64P) for x in where]
+        ws = on.workspace(L.tx_event_attn_workspace_bytes(ctypes.byref(cfg), 0, n, *wp))
+        check(L.tx_event_attn_forward(ctypes.byref(cfg), n, *wp, *map(ctypes.byref, a), ctypes.byref(o), l, M,
+                                      VP(ws.data_ptr()), ws.numel(), on.stream))
+    return out, lse
+
+
+def event_attention_backward(dout, q, k, v, out, lse, key_offsets, event_offsets, query_offsets, prefix_len,
+                             scale: Optional[float] = None, dq=None, dk=None, dv=None, stream=None):
+    """Gradients of event_attention for dout, given its inputs and outputs
+    (tx_event_attn_backward): dq, dk, dv."""
+    where = _event_args(key_offsets, event_offsets, query_offsets, prefix_len)
+    with _On(dict(q=q, k=k, v=v, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv), stream) as on:
+        cfg = _attn_config(q, k, None, scale)
+        M, H = q.shape[0], q.shape[1]
+        _covers(M, where[2], "query")
+        _covers(k.shape[0], where[0], "key")
+        dq = _new_like(q, _whole(where[2], M)) if dq is None else dq
+        dk = _new_like(k, _whole(where[0], k.shape[0])) if dk is None else dk
+        dv = _new_like(v, _whole(where[0], k.shape[0])) if dv is None else dv
+        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype), _heads(v, "v", q.dtype, k.shape)]
+        g = [_heads(dout, "dout", q.dtype, q.shape), _heads(dq, "dq", q.dtype, q.shape),
+             _heads(dk, "dk", q.dtype, k.shape), _heads(dv, "dv", q.dtype, k.shape)]
+        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
+        L, n, wp = lib(), len(where[0]) - 1, [_p(x, I64P) for x in where]
+        ws = on.workspace(L.tx_event_attn_workspace_bytes(ctypes.byref(cfg), 1, n, *wp))
+        check(L.tx_event_attn_backward(ctypes.byref(cfg), n, *wp, *map(ctypes.byref, a), ctypes.byref(o), l, M,
+                                       *map(ctypes.byref, g), VP(ws.data_ptr()), ws.numel(), on.stream))
+    return dq, dk, dv
+
+
+def _pref_args(logits, actions, offsets, beta, smoothing):
+    import torch
+    off = _offsets(offsets, "answer offsets")
+    if len(off) % 2 == 0:
+        _invalid("answer offsets must hold two answers per pair")
+    if logits.dim() not in (1, 2) or (logits.dim() == 2 and logits.shape[1] > 1 and logits.stride(1) != 1):
+        _invalid("logits must be [rows] or [rows, actions] with contiguous actions")
+    if actions.dtype != torch.int32 or tuple(actions.shape) != (logits.shape[0],) or not actions.is_contiguous():
+        _invalid("actions must be a contiguous int32 tensor with an entry per row")
+    if logits.dim() == 2 and logits.shape[1] < 2:
+        _invalid("logits need two actions or more (or [rows] for the scalar head)")
+    _covers(logits.shape[0], off, "answer")
+    k = 1 if logits.dim() == 1 else logits.shape[1]
+    return off, PreferenceConfig(_dtype_of(logits, "logits"), k, float(beta), float(smoothing))
+
+
+def _row_stride(t) -> int:
+    return max(t.stride(0), 1 if t.dim() == 1 else t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def preference_loss(logits, actions, offsets, ref_logp=None, beta: float = 0.1, smoothing: float = 0.0, stream=None):
+    """Preference loss of paired answers (tx_preference_forward). logits [rows]
+    (scalar head) or [rows, actions], actions int32 [rows], offsets of the answers
+    (2p preferred, 2p + 1 not), ref_logp fp32 [answers] or None. Returns loss
+    fp32 [pairs], logp fp32 [answers] and row_lse fp32 [rows] (for the backward)."""
+    import torch
+    with _On(dict(logits=logits, actions=actions, ref_logp=ref_logp), stream) as on:
+        off, cfg = _pref_args(logits, actions, offsets, beta, smoothing)
+        P = len(off) // 2
+        ref = _plain(ref_logp, "ref_logp", torch.float32, (2 * P,)) if ref_logp is not None else VP()
+        loss, logp = (torch.empty(n, dtype=torch.float32, device=on.dev) for n in (P, 2 * P))
+        row_lse = torch.empty(logits.shape[0], dtype=torch.float32, device=on.dev)
+        L, op = lib(), _p(off, I64P)
+        ws = on.workspace(L.tx_preference_workspace_bytes(ctypes.byref(cfg), P, op))
+        check(L.tx_preference_forward(ctypes.byref(cfg), P, op, VP(logits.data_ptr()), _row_stride(logits),
+                                      VP(actions.data_ptr()), ref, VP(loss.data_ptr()), VP(logp.data_ptr()),
+                                      VP(row_lse.data_ptr()), VP(ws.data_ptr()), ws.numel(), on.stream))
+    return loss, logp, row_lse
+
+
+def preference_loss_backward(dloss, logits, actions, offsets, ref_logp, logp, row_lse, beta: float = 0.1,
+                             smoothing: float = 0.0, dlogits=None, stream=None):
+    """d_logits of preference_loss for dloss fp32 [pairs] (tx_preference_backward);
+    rows outside the offsets keep what `dlogits` held (0 where this call makes it)."""
+    import torch
+    with _On(dict(logits=logits, actions=actions, ref_logp=ref_logp, logp=logp, row_lse=row_lse, dloss=dloss,
+                  dlogits=dlogits), stream) as on:
+        off, cfg = _pref_args(logits, actions, offsets, beta, smoothing)
+        P, M = len(off) // 2, logits.shape[0]
+        ref = _plain(ref_logp, "ref_logp", torch.float32, (2 * P,)) if ref_logp is not None else VP()
+        f = [_plain(logp, "logp", torch.float32, (2 * P,)), _plain(row_lse, "row_lse", torch.float32, (M,)),
+             _plain(dloss, "dloss", torch.float32, (P,))]
+        if dlogits is None:
+            dlogits = _new_like(logits, _whole(off, M))
+        if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or \
+                (dlogits.dim() == 2 and dlogits.stride(1) != 1):
+            _invalid("dlogits must be like logits, actions contiguous")
+        L, op = lib(), _p(off, I64P)
+        ws = on.workspace(L.tx_preference_workspace_bytes(ctypes.byref(cfg), P, op))
+        check(L.tx_preference_backward(ctypes.byref(cfg), P, op, VP(logits.data_ptr()), _row_stride(logits),
+                                       VP(actions.data_ptr()), ref, *f, VP(dlogits.data_ptr()), _row_stride(dlogits),
+                                       VP(ws.data_ptr()), ws.numel(), on.stream))
+    return dlogits
 
 
 def profile_enable(on: bool = True):

@@ -1,0 +1,217 @@
+"""rel_attention and its gradients against the 64-bit formulas, each value within
+the bound that its roundings allow (tests/train_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_28940_amd import transx as T
+from tests import train_ref as F
+from tests.parity_util import log
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    torch.cuda.set_device(0)
+
+
+def _off(L, first=0):
+    return (first + np.concatenate([[0], np.cumsum(L)])).astype(np.int64)
+
+
+def _rand(gen, dt, *shape, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dt).cuda()
+
+
+def _inputs(dt, M, H, G, dh, R, seed=0, logits=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v, do = (_rand(gen, dt, M, n, dh, scale=s) for n, s in ((H, logits), (G, 1.0), (G, 1.0), (H, 1.0)))
+    return q, k, v, do, (_rand(gen, dt, H, R, scale=0.7) if R else None)
+
+
+def _step(q, k, v, rel, off, do, **kw):
+    out, lse = T.rel_attention(q, k, v, rel, off, **kw)
+    dq, dk, dv, drel = T.rel_attention_backward(do, q, k, v, rel, out, lse, off, **kw)
+    r = {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+    if drel is not None:
+        r["drel"] = drel
+    return r
+
+
+LENGTHS = [1, 2, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 200, 257]
+
+
+@pytest.mark.parametrize("R", [0, 1, 2, 17, 128, 300])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lengths_around_tiles(dtype, dh, R):
+    dt = DT[dtype]
+    off = _off(LENGTHS)
+    q, k, v, do, rel = _inputs(dt, int(off[-1]), 2, 2, dh, R, seed=dh + R)
+    worst = F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
+    log(f"rel {dtype} d_h {dh} R {R}: {worst}")
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 3), (4, 1), (6, 2), (8, 8)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_head_layouts(dtype, H, G):
+    """Shared key heads, and the tensors as slices of a fused projection, head-major, or rows apart."""
+    dt, dh = DT[dtype], 64
+    off = _off([70, 0, 133, 5])
+    M = int(off[-1])
+    q, k, v, do, rel = _inputs(dt, M, H, G, dh, 40, seed=H)
+    want = F.attention(q, k, v, F.sequences(off), rel, dout=do)
+    plain = _step(q, k, v, rel, off, do)
+    F.check(plain, want)
+    head_major = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, do)]
+    fused = torch.zeros(M, H + 2 * G + 1, dh, dtype=dt, device="cuda")
+    fused[:, :H], fused[:, H:H + G], fused[:, H + G:H + 2 * G] = q, k, v
+    views = (fused[:, :H], fused[:, H:H + G], fused[:, H + G:H + 2 * G])
+    for a, b, c, d in (head_major, views + (do,)):
+        got = _step(a, b, c, rel, off, d)
+        for n in plain:
+            assert torch.equal(got[n], plain[n]), n
+    # gradients into one fused array; what lies beside them stays
+    dfused = torch.full_like(fused, 7.0)
+    out, lse = T.rel_attention(q, k, v, rel, off)
+    T.rel_attention_backward(do, q, k, v, rel, out, lse, off, dq=dfused[:, :H], dk=dfused[:, H:H + G],
+                             dv=dfused[:, H + G:H + 2 * G])
+    assert torch.equal(dfused[:, :H], plain["dq"]) and torch.equal(dfused[:, H:H + G], plain["dk"])
+    assert torch.equal(dfused[:, H + G:H + 2 * G], plain["dv"]) and bool((dfused[:, -1] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 32), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("L", [700, 1500])
+def test_long_sequences_and_split_blocks(dtype, dh, L):
+    """A lone sequence, whose blocks are divided over the card, and large logits."""
+    dt = DT[dtype]
+    off = _off([L])
+    q, k, v, do, rel = _inputs(dt, L, 2, 1, dh, 128, seed=L, logits=3.0)
+    worst = F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
+    log(f"rel {dtype} d_h {dh} L {L}: {worst}")
+
+
+@pytest.mark.parametrize("low", [-float("inf"), -3.3e38, -1e31])
+@pytest.mark.parametrize("dtype,dh", [("f32", 32), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("which", ["near", "middle", "window", "all"])
+def test_masked_buckets(dtype, dh, low, which):
+    dt = DT[dtype]
+    off = _off([300, 1, 64, 129])
+    q, k, v, do, rel = _inputs(dt, int(off[-1]), 2, 2, dh, 48, seed=5)
+    rows = {"near": slice(0, 3), "middle": slice(16, 40), "window": slice(47, 48), "all": slice(0, 48)}[which]
+    rel[:, rows] = low
+    got = _step(q, k, v, rel, off, do)
+    F.check(got, F.attention(q, k, v, F.sequences(off), rel, dout=do))
+    if which in ("near", "all"):  # a sequence's first row sees nothing
+        assert float(got["out"][0].abs().max()) == 0 and float(got["dq"][0].abs().max()) == 0
+        assert bool(torch.isneginf(got["lse"][:, 0]).all())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,dh", [("f32", 64), ("bf16", 64), ("bf16", 128)])
+def test_later_rows_that_are_not_finite(dtype, dh, bad):
+    """A value row that is not finite reaches the rows that see it and no other;
+    neither do not finite keys, queries and gradients of rows that a pair does
+    not join."""
+    dt = DT[dtype]
+    off = _off([150, 90])
+    for name in ("k", "v", "q", "do"):
+        t = dict(zip(("q", "k", "v", "do", "rel"), _inputs(dt, 240, 2, 2, dh, 20, seed=9)))
+        clean = _step(t["q"], t["k"], t["v"], t["rel"], off, t["do"])
+        t[name][100, :, 3] = bad
+        got = _step(t["q"], t["k"], t["v"], t["rel"], off, t["do"])
+        own = slice(100, 150)   # rows that see row 100 (k, v) or are it (q, do: only 100)
+        for n in ("out", "dq"):
+            if name == "do" and n == "out":
+                continue
+            keep = torch.ones(240, dtype=torch.bool, device="cuda")
+            keep[own if name in ("k", "v") else slice(100, 101)] = False
+            assert torch.equal(got[n][keep], clean[n][keep]), (name, n)
+            hit = got[n][~keep]
+            if name == "v" and n == "out":
+                assert not torch.isfinite(hit[:, :, 3]).any()
+                assert torch.equal(hit[:, :, 4], clean[n][~keep][:, :, 4])
+            else:
+                assert not torch.isfinite(hit[:, :, :]).all(), (name, n)
+        for n in ("dk", "dv"):
+            # keys after the last affected query of the sequence, and the other sequence, are as before
+            if name in ("q", "do"):
+                assert torch.equal(got[n][101:], clean[n][101:]), (name, n)
+                assert bool((~torch.isfinite(got[n][:101])).any()) or (name, n) == ("do", "dv") or (name, n) == ("q", "dv")
+            assert torch.equal(got[n][150:], clean[n][150:]), (name, n)
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 32), ("bf16", 128)])
+def test_rows_outside_the_offsets_stay(dtype, dh):
+    dt = DT[dtype]
+    M, off = 200, np.array([13, 90, 90, 150], dtype=np.int64)
+    q, k, v, do, rel = _inputs(dt, M, 2, 2, dh, 16, seed=3)
+    for x in (q, k, v, do):
+        x[:13], x[150:] = float("nan"), float("nan")
+    out, lse = torch.full_like(q, 5.0), torch.full((2, M), 5.0, device="cuda")
+    T.rel_attention(q, k, v, rel, off, out=out, lse=lse)
+    dq, dk, dv = (torch.full_like(x, 5.0) for x in (q, k, v))
+    *_, drel = T.rel_attention_backward(do, q, k, v, rel, out, lse, off, dq=dq, dk=dk, dv=dv)
+    sl = slice(13, 150)
+    want = F.attention(q[sl], k[sl], v[sl], F.sequences(off - 13), rel, dout=do[sl])
+    F.check({"out": out[sl], "lse": lse[:, sl], "dq": dq[sl], "dk": dk[sl], "dv": dv[sl], "drel": drel}, want)
+    for x in (out, dq, dk, dv, lse.t()):
+        assert bool((x[:13] == 5.0).all()) and bool((x[150:] == 5.0).all())
+
+
+def test_empty_calls():
+    q = torch.zeros(0, 2, 32, device="cuda")
+    rel = torch.ones(2, 8, device="cuda")
+    for off in ([0], [0, 0, 0]):
+        out, lse = T.rel_attention(q, q, q, rel, off)
+        dq, dk, dv, drel = T.rel_attention_backward(q, q, q, q, rel, out, lse, off)
+        assert out.shape == q.shape and lse.shape == (2, 0) and bool((drel == 0).all())
+
+
+def test_gradients_by_differences():
+    """Directional derivatives of sum(w out), fp32, by central differences of the 64-bit formula."""
+    off = _off([40, 23])
+    q, k, v, do, rel = _inputs(torch.float32, 63, 2, 1, 32, 12, seed=21)
+    got = _step(q, k, v, rel, off, do)
+    gen = torch.Generator().manual_seed(4)
+    f = lambda *a: float((F.attention(*a[:3], F.sequences(off), a[3])["out"][0] * do.cpu().double()).sum())
+    base = [q.cpu().double(), k.cpu().double(), v.cpu().double(), rel.cpu().double()]
+    for i, n in enumerate(("dq", "dk", "dv", "drel")):
+        d = torch.randn(base[i].shape, generator=gen, dtype=torch.float64)
+        h = 1e-4
+        up, down = ([b + s * h * d if j == i else b for j, b in enumerate(base)] for s in (1, -1))
+        # central differences are off by h^2 / 6 of a third derivative of order 10^2 here
+        want, have = (f(*up) - f(*down)) / (2 * h), float((got[n].cpu().double() * d).sum())
+        assert abs(want - have) <= 2e-5 * (1 + abs(want)), (n, want, have)
+
+
+def test_same_bits_on_every_run_and_in_graphs():
+    off = _off([300, 77, 512])
+    q, k, v, do, rel = _inputs(torch.bfloat16, 889, 4, 2, 64, 64, seed=2)
+    first = _step(q, k, v, rel, off, do)
+    for _ in range(3):
+        again = _step(q, k, v, rel, off, do)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    other = _step(q, k, v, rel, off, do, stream=s)
+    s.synchronize()
+    assert all(torch.equal(first[n], other[n]) for n in first)
+    graphs = []
+    for _ in range(2):  # two graphs, each with workspaces of its own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = _step(q, k, v, rel, off, do)
+        graphs.append((g, res))
+    for turn in range(3):
+        for g, res in graphs:
+            for x in res.values():
+                x.fill_(3.0)
+            g.replay()
+        _step(q * 2, k, v, rel, off, do)
+        torch.cuda.synchronize()
+        for g, res in graphs:
+            assert all(torch.equal(first[n], res[n]) for n in first), turn
