@@ -149,6 +149,21 @@ struct Geo {
 //   cols_mma: acc[f][n] += sum_r tile[r][f] X[r][n], X in the accumulator
 //   layout (lane: column n = lane % 32, register v: row 8 (v / 4) + 4 (lane /
 //   32) + v % 4), which is the layout in which X was computed
+//
+// Scheduling: N fragment reads (R LDS reads each) for N products of M matrix
+// instructions, the reads AHEAD fragments in front; left to itself the
+// compiler hoists all the reads and spills.
+template <int N, int R, int M, int AHEAD = 4>
+__device__ __forceinline__ void pace() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * R, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * M, 0);
+}
+
 template <class T, int DH>
 struct Wave {
   using G = Geo<T, DH>;
@@ -164,8 +179,13 @@ struct Wave {
       col_off = 4 * hi * G::RB + (((l32 >> 2) ^ G::swz(4 * hi)) << 4) + ((l32 & 3) << 2);
     }
   }
+  // Tiles start at multiples of 1024 bytes, so the swizzle's XOR, which stays
+  // within a row, can follow the addition of the tile's address: one addition
+  // for all fragments of a tile.
+  static __device__ __forceinline__ uint32_t lds_address(const lds_char* p) { return (uint32_t)(uintptr_t)p; }
   __device__ __forceinline__ u32x4_t row_frag(const lds_char* tile, int rb, int c) const {
-    return *reinterpret_cast<const lds_u32x4*>(tile + (row_off ^ (c << 5)) + rb * 32 * G::RB);
+    const uint32_t at = (lds_address(tile) + row_off) ^ (c << 5);
+    return *((const lds_u32x4*)(uintptr_t)at + rb * 2 * G::RB);
   }
   static __device__ __forceinline__ floatx16 rows_mma(u32x4_t a, u32x4_t b, floatx16 c) {
     if constexpr (BF) {
@@ -180,10 +200,12 @@ struct Wave {
   }
   // bf16: 8 rows of column 32 db + lane % 32, rows 32 rb + 16 h + 8 (t / 4) + 4 (lane / 32) + t % 4
   __device__ __forceinline__ bf16x8 col_frag(const lds_char* tile, int rb, int h, int db) const {
-    const lds_char* p = tile + (32 * rb + 16 * h) * G::RB;
-    const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (col_off ^ (db << 6))));
-    const s16x4_t b =
-        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * G::RB + (col_off ^ ((db << 6) | (G::swz(8) << 4)))));
+    const uint32_t at = lds_address(tile) + col_off;
+    lds_s16x4* const pa = (lds_s16x4*)(uintptr_t)(at ^ (db << 6)) + (32 * rb + 16 * h) * (G::RB / 8);
+    lds_s16x4* const pb =
+        (lds_s16x4*)(uintptr_t)(at ^ ((db << 6) | (G::swz(8) << 4))) + (32 * rb + 16 * h + 8) * (G::RB / 8);
+    const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(pa);
+    const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(pb);
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
   // fp32: row 32 rb + 8 (v / 4) + 4 (lane / 32) + v % 4 of column 32 db + lane % 32
@@ -208,12 +230,77 @@ struct Wave {
         for (int db = 0; db < G::NB; ++db)
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(tile, rb, h, db), p, acc[db], 0, 0, 0);
       }
+      if constexpr (G::NB >= 2) pace<2 * G::NB, 2, 1>();
     } else {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
 #pragma unroll
         for (int db = 0; db < G::NB; ++db)
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(col_elem(tile, rb, v, db), x[v], acc[db], 0, 0, 0);
+    }
+  }
+  // a = A B^T of the 32 rows rb of a tile, and the same of a second tile
+  __device__ __forceinline__ void rows_product(const lds_char* tile, int rb, const u32x4_t (&f)[G::NC],
+                                               floatx16& a) const {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) a[v] = 0.f;
+#pragma unroll
+    for (int c = 0; c < G::NC; ++c) a = rows_mma(row_frag(tile, rb, c), f[c], a);
+    if constexpr (BF && G::NC >= 4) pace<G::NC, 1, 1>();
+  }
+  __device__ __forceinline__ void rows_products(const lds_char* t1, const u32x4_t (&f1)[G::NC], floatx16& a1,
+                                                const lds_char* t2, const u32x4_t (&f2)[G::NC], floatx16& a2,
+                                                int rb) const {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) a1[v] = 0.f, a2[v] = 0.f;
+#pragma unroll
+    for (int c = 0; c < G::NC; ++c) {
+      a1 = rows_mma(row_frag(t1, rb, c), f1[c], a1);
+      a2 = rows_mma(row_frag(t2, rb, c), f2[c], a2);
+    }
+    if constexpr (BF) pace<2 * G::NC, 1, 1>();
+  }
+  // rows_products with the second operand's fragments of the second product in
+  // LDS too (32 rows at t3)
+  __device__ __forceinline__ void rows_products_lds(const lds_char* t1, const u32x4_t (&f1)[G::NC], floatx16& a1,
+                                                    const lds_char* t2, const lds_char* t3, floatx16& a2,
+                                                    int rb) const {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) a1[v] = 0.f, a2[v] = 0.f;
+#pragma unroll
+    for (int c = 0; c < G::NC; ++c) {
+      a1 = rows_mma(row_frag(t1, rb, c), f1[c], a1);
+      a2 = rows_mma(row_frag(t2, rb, c), row_frag(t3, 0, c), a2);
+    }
+    if constexpr (BF) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < G::NC - 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    }
+  }
+  // cols_mma of two tiles
+  __device__ __forceinline__ void cols_mma2(const lds_char* t1, const floatx16& x1, floatx16 (&acc1)[G::NB],
+                                            const lds_char* t2, const floatx16& x2, floatx16 (&acc2)[G::NB],
+                                            int rb) const {
+    if constexpr (BF) {
+      const bf16x8 p[2] = {pack(x1, 0), pack(x1, 1)}, r[2] = {pack(x2, 0), pack(x2, 1)};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int db = 0; db < G::NB; ++db) {
+          acc1[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(t1, rb, h, db), p[h], acc1[db], 0, 0, 0);
+          acc2[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(t2, rb, h, db), r[h], acc2[db], 0, 0, 0);
+        }
+      pace<4 * G::NB, 2, 1>();
+    } else {
+      cols_mma(t1, rb, x1, acc1);
+      cols_mma(t2, rb, x2, acc2);
     }
   }
   // Whether the 32 rows hold an infinity or a NaN (uniform).
@@ -258,6 +345,7 @@ struct Wave {
       } else {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
+          if (v % 4 == 0) __builtin_amdgcn_sched_barrier(0);
           const float a = col_elem(tile, rb, v, db);
           const bool fin = __builtin_isfinite(a);
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(fin ? a : 0.f, x[v], acc[db], 0, 0, 0);
@@ -266,6 +354,7 @@ struct Wave {
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[db][v] = hit[v] > 0.f ? __builtin_nanf("") : acc[db][v];
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 };

@@ -3,16 +3,29 @@
 // query head that reads the key head. Keys that no query sees get zeros.
 #include "train_attn.h"
 
+#include <type_traits>
+
 namespace tx {
 namespace {
 
-template <class T>
-constexpr int query_tile() { return sizeof(T) == 2 ? 64 : 32; }
+// Rows of a query tile, and whether the block's V rows stay in LDS instead of
+// registers: at d_head 128 the accumulators of dk and dv (128 registers), the K
+// and V fragments (64) and a tile's S and dP do not fit 256 registers, and every
+// spill waits for the tiles in flight. In bf16, V in LDS with 32-row tiles keeps
+// two blocks on a CU (66 KB each): 17.8 -> 4.1 ms for 147 k queries of 2.3 k keys
+// on average. At d_head 64 both stay in registers (216 against 288 us for 17 k
+// queries).
+template <class T, int DH>
+constexpr bool v_in_lds() { return sizeof(T) == 2 && DH == 128; }
+template <class T, int DH>
+constexpr int query_tile() { return sizeof(T) == 2 && DH < 128 ? 64 : 32; }
 
 template <class T, int DH>
-constexpr int dkv_tile_bytes() { return query_tile<T>() * Geo<T, DH>::RB; }
+constexpr int dkv_tile_bytes() { return query_tile<T, DH>() * Geo<T, DH>::RB; }
+template <class T, int DH>
+constexpr int dkv_lds_bytes() { return 4 * dkv_tile_bytes<T, DH>() + (v_in_lds<T, DH>() ? kTrainRows * Geo<T, DH>::RB : 0); }
 
-// A wave owns 32 keys, whose K and V fragments stay in registers. Per 32
+// A wave owns 32 keys, whose K (and V) fragments stay in registers. Per 32
 // queries: S = Q K^T and dP = dO V^T (lanes = keys), P and dS = P (dP - D),
 // then dV^T += dO^T P and dK^T += Q^T dS with P and dS taken from the
 // accumulators and the columns of the dO and Q tiles read from LDS (bf16:
@@ -22,10 +35,11 @@ template <class T, int DH, bool REL>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
-  constexpr int QT = query_tile<T>(), QB = QT / 32, TB = dkv_tile_bytes<T, DH>();
+  constexpr int QT = query_tile<T, DH>(), QB = QT / 32, TB = dkv_tile_bytes<T, DH>();
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
-  lds_float* const stat = (lds_float*)(smem + 4 * TB);  // [2 buffers][lse2, D, limits][QT]
+  lds_char* const sVb = smem + 4 * TB;                               // v_in_lds: the block's V rows
+  lds_float* const stat = (lds_float*)(smem + dkv_lds_bytes<T, DH>());  // [2 buffers][lse2, D, limits][QT]
   lds_float* const tab = stat + 6 * QT;
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int unit = blockIdx.x / a.G, hk = blockIdx.x % a.G, per = a.H / a.G;
@@ -35,20 +49,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
   const bool exists = key < g.nk;
   const int R = REL ? a.R : 0;
 
-  u32x4_t kf[Gm::NC], vf[Gm::NC];
-  load_row_frags<T, DH>(a.k.p + (int64_t)(g.k0 + key) * a.k.row + hk * a.k.head, exists, hi, kf);
-  load_row_frags<T, DH>(a.v.p + (int64_t)(g.k0 + key) * a.v.row + hk * a.v.head, exists, hi, vf);
-
   floatx16 dk[Gm::NB], dv[Gm::NB];
-#pragma unroll
-  for (int db = 0; db < Gm::NB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) dk[db][v] = 0.f, dv[db][v] = 0.f;
 
   // Work list of the block: (query head, query tile), heads outermost. Causal
-  // rows before the block's first key do not see it; with a last bucket that
-  // masks (window), rows more than R - 2 past its last key do not either
-  // (their tiles are masked one by one below, per head).
+  // rows before the block's first key do not see it.
   const int nqt = (g.nq + QT - 1) / QT, t0 = REL ? min(nqt, k_first / QT) : 0, per_head = nqt - t0;
   int i0 = 0, i1 = per * per_head;
   if (parts > 1) {
@@ -56,23 +60,24 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
     i1 = (int)((int64_t)n * (part + 1) / parts);
     i0 = (int)((int64_t)n * part / parts);
   }
-  // next item at or after i whose tile sees the block's keys
-  auto next = [&](int i) {
-    if (!REL) {
-      for (; i < i1; ++i) {
-        const int t = t0 + i % per_head;
-        // QT = 64: one limit tile per query tile; QT = 32: two query tiles per limit tile
-        if (a.tile_lim[g.qt0 + t * QT / kTrainQTile].hi > k_first) break;
-      }
-    }
-    return i;
+  const int R1 = max(R, 1) - 1, k_last = min(g.nk, k_first + kTrainRows) - 1;
+  // causal tiles from t_far on have one bias, the last bucket's
+  const int t_far = REL ? (k_last + R1 + QT - 1) / QT : 0;
+  float far = 0.f;  // the head's last bucket
+  // Class of a query tile: 2 plain (every row sees every key of the block, one
+  // bias), 1 masked or with biases of its own, 0 sees nothing.
+  auto tile_class = [&](int t) {
+    if (REL) return t < t_far ? 1 : far == -INFINITY ? 0 : fabsf(far) < 0x1p20f ? 2 : 1;
+    // (a limit tile covers one query tile of 64 rows or two of 32)
+    const TileLim x = a.tile_lim[g.qt0 + t * QT / kTrainQTile];
+    return x.hi <= k_first ? 0 : x.lo > k_last ? 2 : 1;
   };
-  const W w(lane);
+  const W w0(lane);
   const TileDma<T, DH, QT> qd(wave, lane, a.q.row), dd(wave, lane, a.dO.row);
   // The rows' statistics: threads 0 .. QT - 1 lse, then D, then limits; fetched
   // with the tile, parked in LDS once the tile before has been computed.
-  auto fetch_stat = [&](int i) {
-    const int h = hk * per + i / per_head, r = (t0 + i % per_head) * QT + tid % QT, kind = tid / QT;
+  auto fetch_stat = [&](int h, int t) {
+    const int r = t * QT + tid % QT, kind = tid / QT;
     const bool ok = r < g.nq;
     float x = 0.f;
     if (kind == 0) {
@@ -88,100 +93,125 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
   auto park_stat = [&](float x, int b) {
     if (tid < 3 * QT) stat[b * 3 * QT + tid] = x;
   };
-  auto fetch = [&](int i, int b) {
-    const int h = hk * per + i / per_head, r = (t0 + i % per_head) * QT;
+  auto fetch = [&](int h, int t, int b) {
+    const int r = t * QT;
     qd.load(a.q.p + (int64_t)(g.q0 + r) * a.q.row + h * a.q.head, g.nq - r, smem + b * TB);
     dd.load(a.dO.p + (int64_t)(g.q0 + r) * a.dO.row + h * a.dO.head, g.nq - r, smem + (2 + b) * TB);
   };
-  int i = next(i0), b = 0, h_tab = -1;
-  float far = 0.f;
-  if (i < i1) {
-    fetch(i, 0);
-    park_stat(fetch_stat(i), 0);
-  }
-  while (i < i1) {
-    const int h = hk * per + i / per_head;
-    if (REL && h != h_tab) {
-      // (every wave is past the barrier that ended the last tile of the head before)
-      stage_bias(tab, (const T*)a.rel, R, h, tid);
-      far = bias_value((const T*)a.rel, R, h, max(R, 1) - 1);
-      h_tab = h;
+  // One pass over the work list; STRICT: see train_fwd_kernel.
+  auto pass = [&](auto strict_c) {
+    constexpr bool STRICT = decltype(strict_c)::value, V_LDS = v_in_lds<T, DH>();
+    u32x4_t kf[Gm::NC], vf[V_LDS ? 1 : Gm::NC];
+    load_row_frags<T, DH>(a.k.p + (int64_t)(g.k0 + key) * a.k.row + hk * a.k.head, exists, hi, kf);
+    if constexpr (V_LDS) {
+      const TileDma<T, DH, kTrainRows> vd(wave, lane, a.v.row);
+      vd.load(a.v.p + (int64_t)(g.k0 + k_first) * a.v.row + hk * a.v.head, g.nk - k_first, sVb);
+    } else {
+      load_row_frags<T, DH>(a.v.p + (int64_t)(g.k0 + key) * a.v.row + hk * a.v.head, exists, hi, vf);
     }
-    __syncthreads();
-    const int in = next(i + 1);
-    float st = 0.f;
-    if (in < i1) {
-      fetch(in, b ^ 1);
-      st = fetch_stat(in);
-    }
-    const lds_char* const sQ = smem + b * TB;
-    const lds_char* const sO = smem + (2 + b) * TB;
-    const lds_float* const ss = stat + b * 3 * QT;
-    const int q0 = (t0 + i % per_head) * QT;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const int qr = q0 + 32 * qb;  // first query of the 32
-      if (qr >= g.nq || k_wave >= g.nk) continue;
-      if (REL && qr + 31 < k_wave) continue;
-      const bool near = REL && (qr - (k_wave + 31) < R - 1 || fabsf(far) >= 0x1p20f);
-      if (REL && far == -INFINITY && qr - (k_wave + 31) >= R - 1) continue;
-      floatx16 s, p;
+    for (int db = 0; db < Gm::NB; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = 0.f, p[v] = 0.f;
+      for (int v = 0; v < 16; ++v) dk[db][v] = 0.f, dv[db][v] = 0.f;
+    bool again = false;
+    auto tile = [&](auto masked_c, int t, int b) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+      const lds_char* const sQ = smem + b * TB;
+      const lds_char* const sO = smem + (2 + b) * TB;
+      const lds_float* const ss = stat + b * 3 * QT;
+      // kept from being hoisted: the fragments' addresses are cheaper made anew than held
+      W w = w0;
+      if (V_LDS) asm volatile("" : "+v"(w.row_off), "+v"(w.col_off));
 #pragma unroll
-      for (int c = 0; c < Gm::NC; ++c) s = W::rows_mma(w.row_frag(sQ, qb, c), kf[c], s);
+      for (int qb = 0; qb < QB; ++qb) {
+        const int qr = t * QT + 32 * qb;  // first query of the 32
+        if (MASKED && (qr >= g.nq || (REL && qr + 31 < k_wave))) continue;
+        floatx16 s, p;
+        if constexpr (V_LDS) w.rows_products_lds(sQ, kf, s, sO, sVb + wave * 32 * Gm::RB, p, qb);
+        else w.rows_products(sQ, kf, s, sO, vf, p, qb);
+        if (!MASKED) {
 #pragma unroll
-      for (int c = 0; c < Gm::NC; ++c) p = W::rows_mma(w.row_frag(sO, qb, c), vf[c], p);
-      const int d0 = min(qr - key, R - 1 + kBiasPad - 32) + 4 * hi + kBiasPad;
-      bool masked = near;
-      uint32_t vis = 0xffff;
-      if (!REL) {
-        bool some = false;
-        vis = 0;
+          for (int gq = 0; gq < 4; ++gq) {
+            const floatx4 ls = *reinterpret_cast<const lds_floatx4*>(ss + 32 * qb + 8 * gq + 4 * hi);
+            const floatx4 Dv = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const int v = 4 * gq + t;
+              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, far - ls[t]));
+              p[v] = s[v] * (p[v] - Dv[t]);
+            }
+          }
+          w.cols_mma2(sO, s, dv, sQ, p, dk, qb);
+          continue;
+        }
+        const int d0 = min(qr - key, R1 + kBiasPad - 32) + 4 * hi + kBiasPad;
+        uint32_t vis = 0;
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq) {
-          const floatx4 lm = *reinterpret_cast<const lds_floatx4*>(ss + 2 * QT + 32 * qb + 8 * gq + 4 * hi);
+          const floatx4 ls = *reinterpret_cast<const lds_floatx4*>(ss + 32 * qb + 8 * gq + 4 * hi);
+          const floatx4 Dv = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
+          floatx4 lm = {0.f, 0.f, 0.f, 0.f};
+          if (!REL) lm = *reinterpret_cast<const lds_floatx4*>(ss + 2 * QT + 32 * qb + 8 * gq + 4 * hi);
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const bool see = key < __float_as_int(lm[t]);
-            vis |= see ? 1u << (4 * gq + t) : 0u;
-            some |= !see;
-          }
-        }
-        masked = __any(some);
-      }
-#pragma unroll
-      for (int gq = 0; gq < 4; ++gq) {
-        const floatx4 ls = *reinterpret_cast<const lds_floatx4*>(ss + 32 * qb + 8 * gq + 4 * hi);
-        const floatx4 Dv = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int v = 4 * gq + t;
-          float e;
-          if (masked) {
+            const int v = 4 * gq + t;
             const float bias = REL ? tab[d0 + 8 * gq + t] : 0.f;
-            if (REL && bias == -INFINITY) vis &= ~(1u << v);
+            const bool see = REL ? bias != -INFINITY : key < __float_as_int(lm[t]);
+            vis |= see ? 1u << v : 0u;
             const float lg = fmaf(s[v], a.scale_log2, bias);
-            e = (vis >> v) & 1 ? __builtin_amdgcn_exp2f(lg - ls[t]) : 0.f;
-            p[v] = (vis >> v) & 1 ? e * (p[v] - Dv[t]) : 0.f;
-          } else {
-            e = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, far - ls[t]));
-            p[v] = e * (p[v] - Dv[t]);
+            s[v] = see ? __builtin_amdgcn_exp2f(lg - ls[t]) : 0.f;
+            p[v] = see ? s[v] * (p[v] - Dv[t]) : 0.f;
           }
-          s[v] = e;
+        }
+        if constexpr (STRICT) {
+          w.cols_mma_strict(sO, qb, s, vis, dv);
+          w.cols_mma_strict(sQ, qb, p, vis, dk);
+        } else {
+          again |= w.rows_not_finite(sO, qb) | w.rows_not_finite(sQ, qb);
+          w.cols_mma2(sO, s, dv, sQ, p, dk, qb);
         }
       }
-      if (masked && w.rows_not_finite(sO, qb)) w.cols_mma_strict(sO, qb, s, vis, dv);
-      else w.cols_mma(sO, qb, s, dv);
-      if (masked && w.rows_not_finite(sQ, qb)) w.cols_mma_strict(sQ, qb, p, vis, dk);
-      else w.cols_mma(sQ, qb, p, dk);
+    };
+    // The tiles t .. t1 - 1 of one class of one head, the next one on its way
+    // while one is computed. Ends on a barrier.
+    auto run = [&](auto masked_c, int h, int t, int t1) {
+      constexpr int CLASS = decltype(masked_c)::value ? 1 : 2;
+      auto next = [&](int t) {
+        while (t < t1 && tile_class(t) != CLASS) ++t;
+        return t;
+      };
+      t = next(t);
+      if (t >= t1) return;
+      fetch(h, t, 0);
+      park_stat(fetch_stat(h, t), 0);
+      for (int b = 0; t < t1; b ^= 1) {
+        __syncthreads();
+        const int tn = next(t + 1);
+        float st = 0.f;
+        if (tn < t1) {
+          fetch(h, tn, b ^ 1);
+          st = fetch_stat(h, tn);
+        }
+        if (k_wave < g.nk) tile(masked_c, t, b);
+        if (tn < t1) park_stat(st, b ^ 1);
+        t = tn;
+      }
+      __syncthreads();
+    };
+    for (int hh = 0; hh < per; ++hh) {
+      const int ta = t0 + max(0, i0 - hh * per_head), tb = t0 + min(per_head, i1 - hh * per_head), h = hk * per + hh;
+      if (ta >= tb) continue;
+      if (REL) {
+        // (every wave is past the barrier that ended the head before)
+        stage_bias(tab, (const T*)a.rel, R, h, tid);
+        far = bias_value((const T*)a.rel, R, h, R1);
+      }
+      run(std::false_type{}, h, max(ta, t_far), tb);
+      run(std::true_type{}, h, ta, tb);
     }
-    if (in < i1) park_stat(st, b ^ 1);
-    i = in;
-    b ^= 1;
-    if (REL && i < i1 && hk * per + i / per_head != h_tab) __syncthreads();  // the table changes: all waves are done with it
-  }
-  __syncthreads();  // the tiles are free
+    return again;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
   if (parts > 1) {
     float* const slot =
         a.partial + ((size_t)g.slot_k + (size_t)((kblk * parts + part) * a.G + hk)) * (2 * kTrainRows * DH);
@@ -227,7 +257,7 @@ __global__ __launch_bounds__(256) void train_dkv_merge_kernel(const TrainArgs a)
 
 template <class T, int DH, bool REL>
 hipError_t dkv_launch(const TrainArgs& a, int32_t n_units, hipStream_t s) {
-  const size_t lds = 4 * dkv_tile_bytes<T, DH>() + 6 * 4 * query_tile<T>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
+  const size_t lds = dkv_lds_bytes<T, DH>() + 6 * 4 * query_tile<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void*)train_dkv_kernel<T, DH, REL>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

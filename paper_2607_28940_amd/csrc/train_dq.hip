@@ -9,6 +9,8 @@
 // order.
 #include "train_attn.h"
 
+#include <type_traits>
+
 namespace tx {
 namespace {
 
@@ -44,7 +46,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
   const int qb = REL ? blocks - 1 - local / parts : local / parts;
   const int q_first = qb * kTrainRows;
   const int hk = h / (a.H / a.G);
-  const int R = REL ? a.R : 0, entries = bias_entries(R);
+  const int R = REL ? a.R : 0, R1 = max(R, 1) - 1, entries = bias_entries(R);
   const bool sums = REL && R > 1;
   lds_float* const sub = tab + entries;
 
@@ -57,26 +59,33 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
     if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
-  if (sums)
-    for (int i = tid; i < 8 * entries; i += 256) sub[i] = 0.f;
-  const float far = REL ? bias_value((const T*)a.rel, R, h, max(R, 1) - 1) : 0.f;
+  const float far = REL ? bias_value((const T*)a.rel, R, h, R1) : 0.f;
   int t_begin = 0;
   if (REL && far == -INFINITY) t_begin = max(0, q_first - (R - 2)) / KT;
   int t_end = (k_end + KT - 1) / KT;
+  int t_plain;  // tiles before it: see train_fwd_kernel
+  if (REL) {
+    t_plain = fabsf(far) < 0x1p20f ? max(0, q_first - R1 + 1) / KT : 0;
+  } else {
+    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    t_plain = tl[0].lo;
+    if (q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    t_plain /= KT;
+  }
   if (parts > 1) {
     const int n = max(0, t_end - t_begin);
     t_end = t_begin + (int)((int64_t)n * (part + 1) / parts);
     t_begin += (int)((int64_t)n * part / parts);
   }
+  t_plain = min(t_plain, t_end);
 
   const int q_wave = q_first + wave * 32, q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
   const int64_t row = g.q0 + q_row;
-  u32x4_t qf[Gm::NC], df[Gm::NC];
-  load_row_frags<T, DH>(a.dO.p + row * a.dO.row + h * a.dO.head, exists, hi, df);
   float D = 0.f;
   {
-    u32x4_t of[Gm::NC];
+    u32x4_t of[Gm::NC], df[Gm::NC];
+    load_row_frags<T, DH>(a.dO.p + row * a.dO.row + h * a.dO.head, exists, hi, df);
     load_row_frags<T, DH>(a.o.p + row * a.o.row + h * a.o.head, exists, hi, of);
 #pragma unroll
     for (int c = 0; c < Gm::NC; ++c) {
@@ -92,7 +101,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
     }
     D = xor32_sum(D);
   }
-  load_row_frags<T, DH>(a.q.p + row * a.q.row + h * a.q.head, exists, hi, qf);
   float lse2 = INFINITY;  // a row without visible keys keeps it: its probabilities are 0
   if (exists) {
     const float x = a.lse[(int64_t)h * a.lse_ld + row];
@@ -101,26 +109,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
   }
   int lim = 0;
   if (exists) lim = REL ? q_row + 1 : a.row_lim[row - a.q_base];
-  int lim_lo, lim_hi;
+  int lim_hi = 0;
   if (REL) {
-    lim_lo = q_wave + 1;
-    lim_hi = q_wave >= g.nq ? 0 : min(q_wave + 32, g.nq);
+    if (q_wave < g.nq) lim_hi = min(q_wave + 32, g.nq);
   } else {
-    int lo = exists ? lim : 0x7fffffff, up = lim;
+    int up = lim;
 #pragma unroll
-    for (int m = 1; m < 32; m <<= 1) {
-      lo = min(lo, __shfl_xor(lo, m));
-      up = max(up, __shfl_xor(up, m));
-    }
-    lim_lo = uniform(lo);
+    for (int m = 1; m < 32; m <<= 1) up = max(up, __shfl_xor(up, m));
     lim_hi = uniform(up);
   }
 
   floatx16 dq[Gm::NB];
-#pragma unroll
-  for (int db = 0; db < Gm::NB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
 
   const W w(lane);
   const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
@@ -131,28 +130,31 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
     kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
     vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
   };
-  if (t_begin < t_end) fetch(t_begin, 0);
-  __syncthreads();
-  for (int t = t_begin; t < t_end; ++t) {
-    const int b = (t - t_begin) & 1, k0 = t * KT;
-    if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-    const lds_char* const sK = smem + b * TB;
-    const lds_char* const sV = smem + (2 + b) * TB;
-    if (k0 < lim_hi) {
-      const bool near = REL && (q_wave - (k0 + KT - 1) < R - 1 || fabsf(far) >= 0x1p20f);
-      const bool masked = REL ? near : k0 + KT > lim_lo;
-      const int d0 = min(q_row - k0, R - 1 + kBiasPad - 1) - 4 * hi + kBiasPad;
+  // One pass over the keys; STRICT: see train_fwd_kernel.
+  auto pass = [&](auto strict_c) {
+    constexpr bool STRICT = decltype(strict_c)::value;
+    u32x4_t qf[Gm::NC], df[Gm::NC];
+    load_row_frags<T, DH>(a.dO.p + row * a.dO.row + h * a.dO.head, exists, hi, df);
+    load_row_frags<T, DH>(a.q.p + row * a.q.row + h * a.q.head, exists, hi, qf);
+#pragma unroll
+    for (int db = 0; db < Gm::NB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
+    if (sums)
+      for (int i = tid; i < 8 * entries; i += 256) sub[i] = 0.f;
+    bool again = false;
+    auto tile = [&](auto masked_c, int t, int b) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+      const int k0 = t * KT;
+      const lds_char* const sK = smem + b * TB;
+      const lds_char* const sV = smem + (2 + b) * TB;
+      const int d0 = min(q_row - k0, R1 + kBiasPad - 1) - 4 * hi + kBiasPad;
       const float off = far - lse2;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         floatx16 s, p;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = 0.f, p[v] = 0.f;
-#pragma unroll
-        for (int c = 0; c < Gm::NC; ++c) s = W::rows_mma(w.row_frag(sK, kb, c), qf[c], s);
-#pragma unroll
-        for (int c = 0; c < Gm::NC; ++c) p = W::rows_mma(w.row_frag(sV, kb, c), df[c], p);
-        if (!masked) {
+        w.rows_products(sK, qf, s, sV, df, p, kb);
+        if (!MASKED) {
 #pragma unroll
           for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (p[v] - D);
           w.cols_mma(sK, kb, s, dq);
@@ -169,7 +171,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
           const float lg = fmaf(s[v], a.scale_log2, bias);
           s[v] = see ? __builtin_amdgcn_exp2f(lg - lse2) * (p[v] - D) : 0.f;
         }
-        // (a row past the group's end has lse2 = inf, so it adds 0)
         if (sums) {
           lds_float* const mine = sub + (2 * wave + hi) * entries;
 #pragma unroll
@@ -178,14 +179,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
             if (exists) __builtin_amdgcn_ds_atomic_fadd_f32(mine + (d0 - key), s[v]);
           }
         }
-        if (w.rows_not_finite(sK, kb)) w.cols_mma_strict(sK, kb, s, vis, dq);
-        else w.cols_mma(sK, kb, s, dq);
+        if constexpr (STRICT) {
+          w.cols_mma_strict(sK, kb, s, vis, dq);
+        } else {
+          again |= w.rows_not_finite(sK, kb);
+          w.cols_mma(sK, kb, s, dq);
+        }
       }
-    }
+    };
+    if (t_begin < t_end) fetch(t_begin, 0);
     __syncthreads();
-  }
+    int t = t_begin;
+    const bool rows_here = q_wave < g.nq;
+    for (; t < t_plain; ++t) {
+      const int b = (t - t_begin) & 1;
+      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+      if (rows_here) tile(std::false_type{}, t, b);
+      __syncthreads();
+    }
+    for (; t < t_end; ++t) {
+      const int b = (t - t_begin) & 1;
+      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+      if (t * KT < lim_hi) tile(std::true_type{}, t, b);
+      __syncthreads();
+    }
+    return again;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
   if (sums) {
-    // (the loop, also an empty one, ended on a barrier)
+    // (a pass, also one over no tiles, ends on a barrier)
     float* const out = a.drel_part + ((size_t)unit * a.H + h) * R;
     for (int d = tid; d < R; d += 256) {
       float x = 0.f;

@@ -3,6 +3,8 @@
 // running maximum and sum of the softmax.
 #include "train_attn.h"
 
+#include <type_traits>
+
 namespace tx {
 namespace {
 
@@ -44,48 +46,49 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
     k_end = tl[0].hi;
     if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
-  const int R = REL ? a.R : 0;
+  const int R = REL ? a.R : 0, R1 = max(R, 1) - 1;  // R1: the first distance of the last bucket
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
-  const float far = REL ? bias_value((const T*)a.rel, R, h, max(R, 1) - 1) : 0.f;
+  const float far = REL ? bias_value((const T*)a.rel, R, h, R1) : 0.f;
   int t_begin = 0;
   // a last bucket that masks leaves a window of the R - 1 nearest keys
   if (REL && far == -INFINITY) t_begin = max(0, q_first - (R - 2)) / KT;
   int t_end = (k_end + KT - 1) / KT;
+  // Tiles before t_plain are visible to every row of the block, with one bias
+  // for all pairs; a large one goes to each logit, as there is no telling how
+  // it rounds them.
+  int t_plain;
+  if (REL) {
+    t_plain = fabsf(far) < 0x1p20f ? max(0, q_first - R1 + 1) / KT : 0;
+  } else {
+    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    t_plain = tl[0].lo;
+    if (q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    t_plain /= KT;
+  }
   if (parts > 1) {
     const int n = max(0, t_end - t_begin);
     t_end = t_begin + (int)((int64_t)n * (part + 1) / parts);
     t_begin += (int)((int64_t)n * part / parts);
   }
+  t_plain = min(t_plain, t_end);
 
   const int q_wave = q_first + wave * 32;         // first query of the wave, within the group
   const int q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
-  u32x4_t qf[Gm::NC];
-  load_row_frags<T, DH>(a.q.p + (int64_t)(g.q0 + q_row) * a.q.row + h * a.q.head, exists, hi, qf);
   int lim = 0;  // visible keys of the lane's query
   if (exists) lim = REL ? q_row + 1 : a.row_lim[g.q0 + q_row - a.q_base];
-  int lim_lo, lim_hi;  // over the wave's existing rows
+  int lim_hi = 0;  // the largest of the wave's rows
   if (REL) {
-    lim_lo = q_wave + 1;
-    lim_hi = min(q_wave + 32, g.nq);
-    if (q_wave >= g.nq) lim_hi = 0;
+    if (q_wave < g.nq) lim_hi = min(q_wave + 32, g.nq);
   } else {
-    int lo = exists ? lim : 0x7fffffff, up = lim;
+    int up = lim;
 #pragma unroll
-    for (int m = 1; m < 32; m <<= 1) {
-      lo = min(lo, __shfl_xor(lo, m));
-      up = max(up, __shfl_xor(up, m));
-    }
-    lim_lo = uniform(lo);
+    for (int m = 1; m < 32; m <<= 1) up = max(up, __shfl_xor(up, m));
     lim_hi = uniform(up);
   }
 
   floatx16 o[Gm::NB];
-#pragma unroll
-  for (int db = 0; db < Gm::NB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m, l;
 
   const W w(lane);
   const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
@@ -96,32 +99,37 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
     kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
     vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
   };
-  if (t_begin < t_end) fetch(t_begin, 0);
-  __syncthreads();
-  for (int t = t_begin; t < t_end; ++t) {
-    const int b = (t - t_begin) & 1, k0 = t * KT;
-    if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-    const lds_char* const sK = smem + b * TB;
-    const lds_char* const sV = smem + (2 + b) * TB;
-    if (k0 < lim_hi) {
+  // One pass over the keys. A masked tile whose values are not all finite has
+  // to keep them from the pairs out of sight; that is rare, and its code would
+  // cost every other tile registers, so such a block starts again with STRICT
+  // (same results but for the sums that those values reach).
+  auto pass = [&](auto strict_c) {
+    constexpr bool STRICT = decltype(strict_c)::value;
+    u32x4_t qf[Gm::NC];
+    load_row_frags<T, DH>(a.q.p + (int64_t)(g.q0 + q_row) * a.q.row + h * a.q.head, exists, hi, qf);
+    m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int db = 0; db < Gm::NB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+    bool again = false;
+    // One tile for one wave; MASKED: pairs may be out of sight or near enough for
+    // a bias of their own.
+    auto tile = [&](auto masked_c, int t, int b) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+      const int k0 = t * KT;
+      const lds_char* const sK = smem + b * TB;
+      const lds_char* const sV = smem + (2 + b) * TB;
       floatx16 s[KB];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
-#pragma unroll
-        for (int c = 0; c < Gm::NC; ++c) s[kb] = W::rows_mma(w.row_frag(sK, kb, c), qf[c], s[kb]);
-      }
-      // logits as fma(s, mul, add): plain tiles scale here, tiles that touch the
-      // buckets or the mask were brought to base-2 logits already
-      float mul = a.scale_log2, add = far;
-      const bool near = REL && (q_wave - (k0 + KT - 1) < R - 1 || fabsf(far) >= 0x1p20f);
-      const bool masked = REL ? near : k0 + KT > lim_lo;
-      // the lane's entry of the key 0 of the tile, less its 4 hi: distances beyond the
-      // padding are all in the last bucket
-      const int d0 = min(q_row - k0, R - 1 + kBiasPad - 1) - 4 * hi + kBiasPad;
-      if (masked) {
-        mul = 1.f, add = 0.f;
+      for (int kb = 0; kb < KB; ++kb) w.rows_product(sK, kb, qf, s[kb]);
+      // logits as fma(s, mul, add): plain tiles scale here, masked ones were
+      // brought to base-2 logits already
+      const float mul = MASKED ? 1.f : a.scale_log2, add = MASKED ? 0.f : far;
+      // table entry of the pair with the tile's key 4 hi (distances past the
+      // padding are all in the last bucket)
+      const int d0 = min(q_row - k0, R1 + kBiasPad - 1) - 4 * hi + kBiasPad;
+      if (MASKED) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -141,9 +149,9 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
       mx = fmaf(xor32_max(mx), mul, add);
-      // The reference m moves only when this tile would push a probability
-      // above 2^8 (fine for fp32 sums and for bf16 P, whose rounding is
-      // relative); O / l does not depend on which reference was used.
+      // The reference m moves only when this tile would push a probability above
+      // 2^8 (fine for fp32 sums and for bf16 P, whose rounding is relative); O / l
+      // does not depend on which reference was used.
       const bool bump = mx > m + 8.f;
       if (__any(bump)) {
         const float m_new = bump ? mx : m;
@@ -165,7 +173,8 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
         }
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        if (masked && w.rows_not_finite(sV, kb)) {
+        if (MASKED && !STRICT) again |= w.rows_not_finite(sV, kb);
+        if constexpr (MASKED && STRICT) {
           uint32_t vis = 0;
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
@@ -178,9 +187,26 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
           w.cols_mma(sV, kb, s[kb], o);
         }
       }
-    }
+    };
+    if (t_begin < t_end) fetch(t_begin, 0);
     __syncthreads();
-  }
+    int t = t_begin;
+    const bool rows_here = q_wave < g.nq;
+    for (; t < t_plain; ++t) {
+      const int b = (t - t_begin) & 1;
+      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+      if (rows_here) tile(std::false_type{}, t, b);
+      __syncthreads();
+    }
+    for (; t < t_end; ++t) {
+      const int b = (t - t_begin) & 1;
+      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
+      if (t * KT < lim_hi) tile(std::true_type{}, t, b);
+      __syncthreads();
+    }
+    return again;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
   l = xor32_sum(l);
   if (parts > 1) {
     float* const slot =
