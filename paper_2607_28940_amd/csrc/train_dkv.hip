@@ -64,12 +64,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
   // causal tiles from t_far on have one bias, the last bucket's
   const int t_far = REL ? (k_last + R1 + QT - 1) / QT : 0;
   float far = 0.f;  // the head's last bucket
-  // Class of a query tile: 2 plain (every row sees every key of the block, one
+  // Classes of query tiles: 2 plain (every row sees every key of the block, one
   // bias), 1 masked or with biases of its own, 0 sees nothing.
-  auto tile_class = [&](int t) {
-    if (REL) return t < t_far ? 1 : far == -INFINITY ? 0 : fabsf(far) < 0x1p20f ? 2 : 1;
-    // (a limit tile covers one query tile of 64 rows or two of 32)
-    const TileLim x = a.tile_lim[g.qt0 + t * QT / kTrainQTile];
+  auto tile_class = [&](int t) { return t < t_far ? 1 : far == -INFINITY ? 0 : fabsf(far) < 0x1p20f ? 2 : 1; };
+  auto limit_class = [&](int t) {
+    const TileLim x = a.tile_lim[g.qt0 + t];
     return x.hi <= k_first ? 0 : x.lo > k_last ? 2 : 1;
   };
   const W w0(lane);
@@ -176,9 +175,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
     // while one is computed. Ends on a barrier.
     auto run = [&](auto masked_c, int h, int t, int t1) {
       constexpr int CLASS = decltype(masked_c)::value ? 1 : 2;
+      // the next tile of the class at or after t: causal ones by their index,
+      // event ones from a mask over 64 limit tiles that the wave looks at together
+      int m0 = -64;
+      uint64_t mask = 0;
       auto next = [&](int t) {
-        while (t < t1 && tile_class(t) != CLASS) ++t;
-        return t;
+        if (REL) {
+          while (t < t1 && tile_class(t) != CLASS) ++t;
+          return t;
+        }
+        while (t < t1) {
+          const int lt = t * QT / kTrainQTile;
+          if (lt >= m0 + 64) {
+            m0 = lt;
+            mask = __ballot((lt + lane) * kTrainQTile < g.nq && limit_class(lt + lane) == CLASS);
+          }
+          const uint64_t rest = mask >> (lt - m0);
+          if (rest & 1) break;
+          t = (rest ? lt + __builtin_ctzll(rest) : m0 + 64) * (kTrainQTile / QT);
+        }
+        return min(t, t1);
       };
       t = next(t);
       if (t >= t1) return;

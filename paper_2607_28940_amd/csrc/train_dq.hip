@@ -25,11 +25,38 @@ constexpr int dq_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
 // from the accumulators. dS is rounded to bf16 for that product (relative 2^-9
 // of each term, as P in the forward).
 //
-// Bias gradient: only tiles that touch the buckets below the last one add their
-// dS, per distance, to a padded table in LDS, one per wave and half wave, so
-// that the lanes of one instruction go to different entries and each table is
-// summed in program order. The last bucket needs no sums: every row's dS adds
-// up to zero, so its gradient is minus the sum of the others.
+// Bias gradient: only tiles that touch the buckets below the last one sum their
+// dS by distance; the last bucket needs no sums, since every row's dS adds up
+// to zero: its gradient is minus the sum of the others. Within 32 keys and 32
+// queries the sums are those of the diagonals, 63 of them, made in registers
+// (diagonal_sums) and added to a padded table in LDS, one per wave, so that each
+// table is summed in program order.
+//
+// Sums over the diagonals of a 32 x 32 tile in the accumulator layout (lane:
+// column, registers: rows): lane d gets the sum at column - row = d, lane 64 + d
+// that of d < 0. Rows from the last to the first, each step rotates the sums by
+// a lane and adds a row (T[l] = x_row[l] + T[l + 1]), on a ring of 64 lanes whose
+// upper half starts empty.
+__device__ __forceinline__ float diagonal_sums(const floatx16& x) {
+  constexpr int kWaveRotateLeft = 0x134;
+  float sum = 0.f;
+#pragma unroll
+  for (int g = 3; g >= 0; --g) {
+    float lo[4], up[4];  // rows 8 g + t (lanes 0-31) and 8 g + 4 + t (lanes 32-63), both on lanes 0-31
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[4 * g + t]), 0u, false, false);
+      lo[t] = __uint_as_float(r[0]);
+      up[t] = __uint_as_float(r[1]);
+    }
+#pragma unroll
+    for (int t = 3; t >= 0; --t) sum = up[t] + dpp_f32<kWaveRotateLeft>(sum);
+#pragma unroll
+    for (int t = 3; t >= 0; --t) sum = lo[t] + dpp_f32<kWaveRotateLeft>(sum);
+  }
+  return sum;
+}
+
 template <class T, int DH, bool REL>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
@@ -141,7 +168,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
 #pragma unroll
       for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
     if (sums)
-      for (int i = tid; i < 8 * entries; i += 256) sub[i] = 0.f;
+      for (int i = tid; i < 4 * entries; i += 256) sub[i] = 0.f;
     bool again = false;
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
@@ -172,12 +199,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
           s[v] = see ? __builtin_amdgcn_exp2f(lg - lse2) * (p[v] - D) : 0.f;
         }
         if (sums) {
-          lds_float* const mine = sub + (2 * wave + hi) * entries;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int key = kb * 32 + 8 * (v >> 2) + (v & 3);
-            if (exists) __builtin_amdgcn_ds_atomic_fadd_f32(mine + (d0 - key), s[v]);
-          }
+          // lane d (or 64 + d): distance q_wave - k0 - 32 kb + d; past the padding nothing is kept
+          const int at = q_wave - k0 - 32 * kb + (lane < 32 ? lane : lane - 64) + kBiasPad;
+          const float x = diagonal_sums(s);
+          if (at >= 0 && at < entries) __builtin_amdgcn_ds_atomic_fadd_f32(sub + wave * entries + at, x);
         }
         if constexpr (STRICT) {
           w.cols_mma_strict(sK, kb, s, vis, dq);
@@ -213,7 +238,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
       float x = 0.f;
       if (d < R - 1)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x += sub[i * entries + kBiasPad + d];
+        for (int i = 0; i < 4; ++i) x += sub[i * entries + kBiasPad + d];
       out[d] = x;
     }
   }
@@ -282,7 +307,7 @@ __global__ __launch_bounds__(256) void drel_head_kernel(const float* __restrict_
 
 template <class T, int DH, bool REL>
 hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
-  const size_t lds = 4 * dq_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 9 : 1) : 0);
+  const size_t lds = 4 * dq_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 5 : 1) : 0);
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void*)train_dq_kernel<T, DH, REL>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
