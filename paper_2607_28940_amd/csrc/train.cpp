@@ -116,7 +116,7 @@ struct AttnPlan {
   size_t o_row = 0, o_prefix = 0;
   size_t bytes = 0;
   struct {
-    size_t row_lim, tile_lim, D, partial, drel, drel2;
+    size_t row_lim, tile_lim, stat, partial, drel, drel2;
   } at;
 };
 
@@ -190,9 +190,9 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
     return cv.off - n;
   };
   take(p.meta.size());
-  p.at.row_lim = take(rel ? 0 : p.rows_q * 4);
+  p.at.row_lim = take(rel ? 0 : (p.rows_q + 1) * 4);
   p.at.tile_lim = take(rel ? 0 : p.tiles * sizeof(TileLim));
-  p.at.D = take(backward ? (size_t)H * p.rows_q * 4 : 0);
+  p.at.stat = take(backward ? (size_t)H * p.rows_q * 8 : 0);
   // dq and then dk, dv use the slots in turn
   const size_t sq = p.slots_q * (backward ? train_dq_slot(dh) : train_fwd_slot(dh));
   const size_t sk = backward ? p.slots_k * train_dkv_slot(dh) : 0;
@@ -306,8 +306,8 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   a.H = H, a.G = G;
   a.lse = x.lse;
   a.lse_ld = x.lse_stride;
-  a.D_ld = p.rows_q;
-  a.D = (float*)(w + p.at.D);
+  a.stat_ld = p.rows_q;
+  a.row_stat = (float*)(w + p.at.stat);
   a.rel = x.rel;
   a.R = R;
   a.row_lim = (const int32_t*)(w + p.at.row_lim);

@@ -53,11 +53,12 @@ struct TrainArgs {
   HeadRows q, k, v, o, dO, dq, dk, dv;
   float* lse;           // [H][lse_ld], natural logarithm
   int64_t lse_ld;
-  float* D;             // [H][D_ld], from row q_base on
-  int64_t D_ld;
+  float* row_stat;      // [H][stat_ld][2]: lse in base 2 (infinite for a row that sees nothing) and D, from
+                        // row q_base on; dq writes them, dk and dv read them
+  int64_t stat_ld;
   const void* rel;      // [H][R] in the tensors' type
   int32_t R;
-  const int32_t* row_lim;   // event form: visible keys of each query row (from row q_base on)
+  const int32_t* row_lim;   // event form: visible keys of each query row (from row q_base on; room for an even number)
   const TileLim* tile_lim;
   int32_t q_base;
   float scale, scale_log2;
@@ -94,7 +95,6 @@ constexpr int kBiasPad = 96;
 __host__ __device__ inline int bias_entries(int R) { return R + 2 * kBiasPad; }
 
 typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) void lds_void;
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
@@ -363,30 +363,53 @@ struct Wave {
 // from HBM/L2 (no registers), by the four waves of a block: piece p (1 KB of
 // the tile) goes to wave p % 4. Rows past `rows` read as zeros (they lie beyond
 // the buffer resource's extent). The swizzle is applied on the global side.
-template <class T, int DH, int ROWS>
+//
+// The loads are written in asm (they have no result registers; the LDS address
+// of the wave's 1 KB is in m0): behind the builtin the compiler makes every
+// transposing LDS read wait for all loads in flight, the next tile's among
+// them. So nothing waits for them but tiles_ready().
+// HELD: the lane's offsets stay in registers; otherwise they are made anew for
+// every tile.
+template <class T, int DH, int ROWS, bool HELD = true>
 struct TileDma {
   using G = Geo<T, DH>;
   static constexpr int PER = ROWS * G::RB / 4096;  // pieces of a wave
-  uint32_t off[PER];
-  int wave;
+  uint32_t off[HELD ? PER : 1];
+  int wave, lane;
   uint32_t ldb;
-  __device__ __forceinline__ TileDma(int wave_, int lane, int64_t row_bytes) : wave(wave_), ldb((uint32_t)row_bytes) {
+  __device__ __forceinline__ uint32_t offset(int u, int l) const {
+    const int r = (wave + 4 * u) * (1024 / G::RB) + l / G::UPR, s = l % G::UPR;
+    return (uint32_t)r * ldb + ((uint32_t)(s ^ G::swz(r)) << 4);
+  }
+  __device__ __forceinline__ TileDma(int wave_, int lane_, int64_t row_bytes)
+      : wave(wave_), lane(lane_), ldb((uint32_t)row_bytes) {
+    if (HELD)
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int r = (wave + 4 * u) * (1024 / G::RB) + lane / G::UPR, s = lane % G::UPR;
-      off[u] = (uint32_t)r * ldb + ((uint32_t)(s ^ G::swz(r)) << 4);
-    }
+      for (int u = 0; u < PER; ++u) off[u] = offset(u, lane);
   }
   // rows: rows left in the tensor's group from `first` on (>= 1)
   __device__ __forceinline__ void load(const char* first, int rows, lds_char* tile) const {
     const int n = min(rows, ROWS);
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)((uint32_t)(n - 1) * ldb + G::RB), 0x00020000);
+    const uint64_t at = (uint64_t)first;
+    const u32x4_t r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)(n - 1) * ldb + G::RB, 0x00020000u};
+    const uint32_t to = uniform((int)(uint32_t)(uintptr_t)tile) + wave * 1024;
+    int l = lane;
+    if (!HELD) asm volatile("" : "+v"(l));  // not hoisted
 #pragma unroll
     for (int u = 0; u < PER; ++u)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + (wave + 4 * u) * 1024), 16, (int)off[u], 0, 0, 0);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :
+                   : "s"(to + u * 4096), "v"(HELD ? off[HELD ? u : 0] : offset(u, l)), "s"(r)
+                   : "m0", "memory");
   }
 };
+
+// Every wave's copies into LDS have landed and every wave is past its last reads.
+__device__ __forceinline__ void tiles_ready() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
+  __syncthreads();
+}
 
 // The lane's fragments of one row (lane % 32) straight from memory; zeros
 // where the row does not exist.
@@ -398,6 +421,19 @@ __device__ __forceinline__ void load_row_frags(const char* row, bool exists, int
 #pragma unroll
     for (int c = 0; c < Geo<T, DH>::NC; ++c) f[c] = *reinterpret_cast<const u32x4_t*>(row + 32 * c + 16 * hi);
   }
+}
+
+// Waits for values loaded from memory: left to the compiler, the wait would sit
+// at their first use, inside a loop over tiles, where it would also wait for the
+// tiles in flight.
+template <int N>
+__device__ __forceinline__ void pin(u32x4_t (&f)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) asm volatile("" : "+v"(f[c]));
+}
+template <class T>
+__device__ __forceinline__ void pin(T& x) {
+  asm volatile("" : "+v"(x));
 }
 
 // Parks a wave's accumulator (columns = rows of the output, 32 of them) in LDS

@@ -71,26 +71,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
     const TileLim x = a.tile_lim[g.qt0 + t];
     return x.hi <= k_first ? 0 : x.lo > k_last ? 2 : 1;
   };
-  const W w0(lane);
-  const TileDma<T, DH, QT> qd(wave, lane, a.q.row), dd(wave, lane, a.dO.row);
-  // The rows' statistics: threads 0 .. QT - 1 lse, then D, then limits; fetched
-  // with the tile, parked in LDS once the tile before has been computed.
+  const TileDma<T, DH, QT, !v_in_lds<T, DH>()> qd(wave, lane, a.q.row), dd(wave, lane, a.dO.row);
+  // The rows' statistics: threads 0 .. QT - 1 fetch lse and D, the next QT the
+  // limits, with the tile (rows past the last one read the last); they are parked
+  // in LDS once the tile before has been computed, and nothing touches them till
+  // then, as that would wait for the tile too.
+  typedef float float2_t __attribute__((ext_vector_type(2)));
   auto fetch_stat = [&](int h, int t) {
-    const int r = t * QT + tid % QT, kind = tid / QT;
-    const bool ok = r < g.nq;
-    float x = 0.f;
-    if (kind == 0) {
-      x = ok ? a.lse[(int64_t)h * a.lse_ld + g.q0 + r] : -INFINITY;
-      x = x == -INFINITY ? INFINITY : x * kTrainLog2e;  // probabilities 0 for rows that see nothing
-    } else if (kind == 1) {
-      x = ok ? a.D[(int64_t)h * a.D_ld + g.q0 + r - a.q_base] : 0.f;
-    } else if (kind == 2 && !REL) {
-      x = __int_as_float(ok ? a.row_lim[g.q0 + r - a.q_base] : 0);
-    }
-    return x;
+    int id = tid;
+    asm volatile("" : "+v"(id));  // not hoisted
+    const int64_t r = g.q0 + min(t * QT + id % QT, g.nq - 1) - a.q_base;
+    const float2_t* p = (const float2_t*)a.row_stat + (h * a.stat_ld + r);
+    if (!REL && id >= QT) p = (const float2_t*)(a.row_lim + (r & ~1));
+    return *p;
   };
-  auto park_stat = [&](float x, int b) {
-    if (tid < 3 * QT) stat[b * 3 * QT + tid] = x;
+  auto park_stat = [&](float2_t x, int t, int b) {
+    int id = tid;
+    asm volatile("" : "+v"(id));
+    const int r = t * QT + id % QT;
+    const bool ok = r < g.nq;
+    lds_float* const to = stat + b * 3 * QT + id;
+    if (id < QT) {
+      to[0] = ok ? x[0] : INFINITY;  // probabilities 0
+      to[QT] = ok ? x[1] : 0.f;
+    } else if (!REL && id < 2 * QT) {
+      to[QT] = ok ? ((g.q0 + r - a.q_base) & 1 ? x[1] : x[0]) : 0.f;
+    }
   };
   auto fetch = [&](int h, int t, int b) {
     const int r = t * QT;
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
     u32x4_t kf[Gm::NC], vf[V_LDS ? 1 : Gm::NC];
     load_row_frags<T, DH>(a.k.p + (int64_t)(g.k0 + key) * a.k.row + hk * a.k.head, exists, hi, kf);
     if constexpr (V_LDS) {
-      const TileDma<T, DH, kTrainRows> vd(wave, lane, a.v.row);
+      const TileDma<T, DH, kTrainRows, false> vd(wave, lane, a.v.row);
       vd.load(a.v.p + (int64_t)(g.k0 + k_first) * a.v.row + hk * a.v.head, g.nk - k_first, sVb);
     } else {
       load_row_frags<T, DH>(a.v.p + (int64_t)(g.k0 + key) * a.v.row + hk * a.v.head, exists, hi, vf);
@@ -112,15 +118,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
     for (int db = 0; db < Gm::NB; ++db)
 #pragma unroll
       for (int v = 0; v < 16; ++v) dk[db][v] = 0.f, dv[db][v] = 0.f;
+    pin(kf);
+    if (!V_LDS) pin(vf);
     bool again = false;
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
       const lds_char* const sQ = smem + b * TB;
       const lds_char* const sO = smem + (2 + b) * TB;
       const lds_float* const ss = stat + b * 3 * QT;
-      // kept from being hoisted: the fragments' addresses are cheaper made anew than held
-      W w = w0;
-      if (V_LDS) asm volatile("" : "+v"(w.row_off), "+v"(w.col_off));
+      // at d_head 128 the fragments' addresses are cheaper made anew than held
+      int id = tid;
+      if (V_LDS) asm volatile("" : "+v"(id));  // not hoisted
+      const W w(id & 63);
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         const int qr = t * QT + 32 * qb;  // first query of the 32
@@ -199,17 +208,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
       t = next(t);
       if (t >= t1) return;
       fetch(h, t, 0);
-      park_stat(fetch_stat(h, t), 0);
+      park_stat(fetch_stat(h, t), t, 0);
       for (int b = 0; t < t1; b ^= 1) {
-        __syncthreads();
+        tiles_ready();
         const int tn = next(t + 1);
-        float st = 0.f;
+        float2_t st = {0.f, 0.f};
         if (tn < t1) {
           fetch(h, tn, b ^ 1);
           st = fetch_stat(h, tn);
         }
         if (k_wave < g.nk) tile(masked_c, t, b);
-        if (tn < t1) park_stat(st, b ^ 1);
+        if (tn < t1) park_stat(st, tn, b ^ 1);
         t = tn;
       }
       __syncthreads();

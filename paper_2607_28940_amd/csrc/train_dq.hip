@@ -132,7 +132,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
   if (exists) {
     const float x = a.lse[(int64_t)h * a.lse_ld + row];
     if (x != -INFINITY) lse2 = x * kTrainLog2e;
-    if (part == 0 && hi == 0) a.D[(int64_t)h * a.D_ld + row - a.q_base] = D;
+    if (part == 0 && hi == 0) {
+      float* const st = a.row_stat + 2 * ((int64_t)h * a.stat_ld + row - a.q_base);
+      st[0] = lse2;
+      st[1] = D;
+    }
   }
   int lim = 0;
   if (exists) lim = REL ? q_row + 1 : a.row_lim[row - a.q_base];
@@ -213,20 +217,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
       }
     };
     if (t_begin < t_end) fetch(t_begin, 0);
-    __syncthreads();
+    pin(qf), pin(df), pin(lim), pin(lse2), pin(D);
+    tiles_ready();
     int t = t_begin;
     const bool rows_here = q_wave < g.nq;
     for (; t < t_plain; ++t) {
       const int b = (t - t_begin) & 1;
       if (t + 1 < t_end) fetch(t + 1, b ^ 1);
       if (rows_here) tile(std::false_type{}, t, b);
-      __syncthreads();
+      tiles_ready();
     }
     for (; t < t_end; ++t) {
       const int b = (t - t_begin) & 1;
       if (t + 1 < t_end) fetch(t + 1, b ^ 1);
       if (t * KT < lim_hi) tile(std::true_type{}, t, b);
-      __syncthreads();
+      tiles_ready();
     }
     return again;
   };

@@ -189,20 +189,21 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
       }
     };
     if (t_begin < t_end) fetch(t_begin, 0);
-    __syncthreads();
+    pin(qf), pin(lim);
+    tiles_ready();
     int t = t_begin;
     const bool rows_here = q_wave < g.nq;
     for (; t < t_plain; ++t) {
       const int b = (t - t_begin) & 1;
       if (t + 1 < t_end) fetch(t + 1, b ^ 1);
       if (rows_here) tile(std::false_type{}, t, b);
-      __syncthreads();
+      tiles_ready();
     }
     for (; t < t_end; ++t) {
       const int b = (t - t_begin) & 1;
       if (t + 1 < t_end) fetch(t + 1, b ^ 1);
       if (t * KT < lim_hi) tile(std::true_type{}, t, b);
-      __syncthreads();
+      tiles_ready();
     }
     return again;
   };
