@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -25,6 +26,7 @@ constexpr int64_t kMaxRows = 0x7fffffff - 4096;
 // Blocks that fill the card (256 CUs, two resident blocks each).
 constexpr int64_t kFullGrid = 512;
 constexpr int kMaxParts = 64;
+int kMinSteps = getenv("TXMIN") ? atoi(getenv("TXMIN")) : 4;  // EXPERIMENT
 
 // Metadata goes up as kernel arguments, 3 KB a launch: no staging buffer whose
 // reuse would have to wait, and a captured graph keeps its own copy.
@@ -126,9 +128,11 @@ struct AttnPlan {
 // part below min_steps, where writing and joining partial results costs more
 // than it saves.
 int parts_of(int64_t steps, int64_t total_steps, int min_steps) {
-  const int64_t target = std::max<int64_t>(min_steps, (total_steps + kFullGrid - 1) / kFullGrid);
-  if (steps < 2 * target) return 1;
-  return (int)std::min<int64_t>(kMaxParts, steps / target);
+  static int slots = getenv("TXSLOTS") ? atoi(getenv("TXSLOTS")) : 512;  // EXPERIMENT
+  static int pct = getenv("TXPCT") ? atoi(getenv("TXPCT")) : 200;  // EXPERIMENT
+  const int64_t target = std::max<int64_t>(min_steps, (total_steps + slots - 1) / slots);
+  if (steps * 100 < target * pct) return 1;
+  return (int)std::min<int64_t>(kMaxParts, (steps + target - 1) / target);
 }
 
 int64_t blocks_of(int64_t rows) { return (rows + kTrainRows - 1) / kTrainRows; }
@@ -162,14 +166,14 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   }
   for (size_t i = 0; i < p.groups.size(); ++i) {
     TrainGroup& g = p.groups[i];
-    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, 4) : 1;
+    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, kMinSteps) : 1;
     g.unit_q = (int32_t)p.units_q;
     g.slot_q = (int32_t)p.slots_q;
     g.qt0 = (int32_t)p.tiles;
     p.units_q += blocks_of(g.nq) * g.parts_q;
     if (g.parts_q > 1) p.slots_q += blocks_of(g.nq) * g.parts_q * H;
     p.tiles += tiles_of(g.nq);
-    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * (H / G), steps_k, 4) : 1;
+    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * (H / G), steps_k, kMinSteps) : 1;
     g.unit_k = (int32_t)p.units_k;
     g.slot_k = (int32_t)p.slots_k;
     p.units_k += blocks_of(g.nk) * g.parts_k;
@@ -199,7 +203,7 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   p.at.partial = take(std::max(sq, sk) * 4);
   const size_t HR = rel && backward ? (size_t)H * c.rel_pos_buckets : 0;
   p.at.drel = take(HR * p.units_q * 4);
-  p.at.drel2 = take(HR * ((p.units_q + 63) / 64) * 4);
+  p.at.drel2 = take(HR * ((p.units_q + 31) / 32) * 4);
   p.bytes = align_up(cv.off + 256);
 }
 
@@ -326,18 +330,16 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   const double stat = 4.0 * H * p.rows_q;
   if (!backward) {
     TX_LAUNCH(K_TRAIN_FWD, 2 * prod, 2 * qb + 2 * kb + stat, launch_train_fwd(bf, dh, rel, a, st));
-    if (p.slots_q) TX_LAUNCH(K_TRAIN_FWD, 0, 0, launch_train_fwd_merge(bf, dh, a, st));
+    if (p.slots_q) TX_LAUNCH(K_TRAIN_FWD, 0, 0, launch_train_fwd_join(bf, dh, a, st));
     return TX_OK;
   }
-  if (p.units_q) {
-    TX_LAUNCH(K_TRAIN_DQ, 3 * prod, 4 * qb + 2 * kb + 2 * stat, launch_train_dq(bf, dh, rel, a, st));
-    if (p.slots_q) TX_LAUNCH(K_TRAIN_DQ, 0, 0, launch_train_dq_merge(bf, dh, a, st));
-  }
+  if (p.units_q) TX_LAUNCH(K_TRAIN_DQ, 3 * prod, 4 * qb + 2 * kb + 2 * stat, launch_train_dq(bf, dh, rel, a, st));
+  if (p.slots_q) TX_LAUNCH(K_TRAIN_DQ, 0, 0, launch_train_dq_join(bf, dh, a, st));
   if (drel) TX_LAUNCH(K_TRAIN_DQ, 0, 0, launch_train_drel(bf, a, (float*)(w + p.at.drel2), x.d_rel, st));
-  if (p.units_k) {
-    TX_LAUNCH(K_TRAIN_DKV, 4 * prod, 2 * qb + 4 * kb + 2 * stat, launch_train_dkv(bf, dh, rel, a, (int32_t)p.units_k, st));
-    if (p.slots_k) TX_LAUNCH(K_TRAIN_DKV, 0, 0, launch_train_dkv_merge(bf, dh, a, (int32_t)p.units_k, st));
-  }
+  if (p.units_k)
+    TX_LAUNCH(K_TRAIN_DKV, 4 * prod, 2 * qb + 4 * kb + 2 * stat,
+              launch_train_dkv(bf, dh, rel, a, (int32_t)p.units_k, st));
+  if (p.slots_k) TX_LAUNCH(K_TRAIN_DKV, 0, 0, launch_train_dkv_join(bf, dh, a, (int32_t)p.units_k, st));
   return TX_OK;
 }
 

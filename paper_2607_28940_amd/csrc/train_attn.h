@@ -24,7 +24,10 @@ namespace tx {
 // the group owns units unit_q .. , parts_q per block of kTrainRows queries, for
 // the key-side launch (dk, dv) unit_k .. , parts_k per block of kTrainRows
 // keys. Groups whose blocks are divided (parts > 1) keep their partial results
-// in slots from slot_q / slot_k on. qt0: its first entry in the 64-row query
+// in slots from slot_q / slot_k on, which a second launch joins in the order of
+// the parts (joining them in the block that finishes last saves that launch,
+// but the fences write whole L2 caches back: one token against 4096 keys took
+// 131 us so, of 64 parts a head). qt0: its first entry in the 64-row query
 // tile list; e0 .. e1 - 1: its events.
 struct TrainGroup {
   int32_t q0, nq, k0, nk;
@@ -67,12 +70,12 @@ struct TrainArgs {
 };
 
 hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
-hipError_t launch_train_fwd_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_fwd_join(bool bf, int dh, const TrainArgs& a, hipStream_t s);
 hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
-hipError_t launch_train_dq_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_dq_join(bool bf, int dh, const TrainArgs& a, hipStream_t s);
 hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
-hipError_t launch_train_dkv_merge(bool bf, int dh, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
-// drel[h][b] from the units' sums; scratch: [chunks][H][R] floats, chunks = ceil(units / 64)
+hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
+// drel[h][b] from the units' sums; scratch: [chunks][H][R] floats, chunks = ceil(units / 32)
 hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s);
 // row_lim and tile_lim of the event form from the events' row offsets and prefixes
 hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
@@ -484,6 +487,58 @@ __device__ __forceinline__ void store_partial(const floatx16 (&acc)[Geo<T, DH>::
       for (int t = 0; t < 4; ++t) w[t] = acc[db][4 * gq + t];
       *reinterpret_cast<floatx4*>(row + 32 * db + 8 * gq + 4 * hi) = w;
     }
+}
+
+// How a block of 256 threads goes through `rows` partial rows of DH floats: DH /
+// 4 threads a row, as many rows at once as there are threads or rows, and what
+// threads are left over on shares of the parts.
+template <int DH>
+struct Joiner {
+  static constexpr int LPR = DH / 4, GROUPS = 256 / LPR;
+  int f, slot, share, at_once, shares;
+  __device__ __forceinline__ Joiner(int rows, int tid) {
+    at_once = 1;
+    while (at_once < rows && at_once < GROUPS) at_once <<= 1;
+    shares = GROUPS / at_once;
+    f = tid % LPR * 4;
+    slot = tid / LPR % at_once;
+    share = tid / LPR / at_once;
+  }
+};
+
+// out[r] = mul * sum over the parts of rows r of their slots (step floats apart).
+template <class T, int DH>
+__device__ __forceinline__ void join_sums(const float* p0, size_t step, int parts, int rows, float mul, char* out,
+                                          int64_t row_bytes, lds_char* smem, int tid) {
+  const Joiner<DH> j(rows, tid);
+  lds_floatx4* const left = (lds_floatx4*)smem;
+  for (int r0 = 0; r0 < rows; r0 += j.at_once) {
+    const int r = r0 + j.slot;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (r < rows) {
+#pragma unroll 4
+      for (int p = j.share; p < parts; p += j.shares) {
+        const floatx4 x = *reinterpret_cast<const floatx4*>(p0 + p * step + (size_t)r * DH + j.f);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] += x[t];
+      }
+    }
+    if (j.shares > 1) {
+      left[tid] = acc;
+      __syncthreads();
+      for (int q = 1; q < j.shares && j.share == 0; ++q) {
+        const floatx4 x = left[tid + q * j.at_once * Joiner<DH>::LPR];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] += x[t];
+      }
+      __syncthreads();
+    }
+    if (r < rows && j.share == 0) {
+      T* const to = (T*)(out + r * row_bytes) + j.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) to[t] = (T)(acc[t] * mul);
+    }
+  }
 }
 
 // The head's bias in base-2 units, padded: entry kBiasPad + d is the bias of

@@ -13,10 +13,11 @@ namespace {
 // and V fragments (64) and a tile's S and dP do not fit 256 registers, and every
 // spill waits for the tiles in flight. In bf16, V in LDS with 32-row tiles keeps
 // two blocks on a CU (66 KB each): 17.8 -> 4.1 ms for 147 k queries of 2.3 k keys
-// on average. At d_head 64 both stay in registers (216 against 288 us for 17 k
-// queries).
+// on average. At d_head 64 V in LDS lets three blocks of 168 registers share a CU
+// (1.16 against 1.24 ms for 111 k queries of 2.3 k keys with two), at 32 it fits
+// registers four times over.
 template <class T, int DH>
-constexpr bool v_in_lds() { return sizeof(T) == 2 && DH == 128; }
+constexpr bool v_in_lds() { return sizeof(T) == 2 && DH >= 64; }
 template <class T, int DH>
 constexpr int query_tile() { return sizeof(T) == 2 && DH < 128 ? 64 : 32; }
 
@@ -32,7 +33,7 @@ constexpr int dkv_lds_bytes() { return 4 * dkv_tile_bytes<T, DH>() + (v_in_lds<T
 // transposing reads). P and dS are rounded to bf16 for those products. Q, dO
 // and the rows' lse, D and key limits are double-buffered, one barrier a tile.
 template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4) void train_dkv_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
   constexpr int QT = query_tile<T, DH>(), QB = QT / 32, TB = dkv_tile_bytes<T, DH>();
@@ -254,30 +255,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dkv_kernel(
 }
 
 template <class T, int DH>
-__global__ __launch_bounds__(256) void train_dkv_merge_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256) void train_dkv_join_kernel(const TrainArgs a) {
+  __shared__ __align__(16) char left_[256 * 16];
+  lds_char* const left = (lds_char*)left_;
   const int unit = blockIdx.x / a.G, hk = blockIdx.x % a.G, tid = threadIdx.x;
   const TrainGroup g = a.groups[find_group<true>(a.groups, a.n_groups, unit, tid & 63)];
-  const int parts = g.parts_k, local = unit - g.unit_k;
+  const int parts = g.parts_k, local = unit - g.unit_k, kblk = local / parts, k_first = kblk * kTrainRows;
   if (parts == 1 || local % parts) return;
-  const int kblk = local / parts, rows = min(kTrainRows, g.nk - kblk * kTrainRows);
-  constexpr size_t SLOT = (size_t)2 * kTrainRows * DH;
-  const float* const p0 = a.partial + ((size_t)g.slot_k + (size_t)(kblk * parts * a.G + hk)) * SLOT;
-  constexpr int LPR = DH / 4;
-  for (int i = tid; i < 2 * rows * LPR; i += 256) {
-    const int which = i / (rows * LPR), j = i % (rows * LPR), r = j / LPR, f = j % LPR * 4;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-      const floatx4 x =
-          *reinterpret_cast<const floatx4*>(p0 + p * SLOT * a.G + (size_t)(which * kTrainRows + r) * DH + f);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] += x[t];
-    }
-    const HeadRows& d = which ? a.dv : a.dk;
-    const float mul = which ? 1.f : a.scale;
-    T* const out = (T*)(d.p + (int64_t)(g.k0 + kblk * kTrainRows + r) * d.row + hk * d.head) + f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * mul);
-  }
+  const float* const p0 = a.partial + ((size_t)g.slot_k + (size_t)(kblk * parts * a.G + hk)) * (2 * kTrainRows * DH);
+  const size_t step = (size_t)a.G * 2 * kTrainRows * DH;
+  const int rows = min(kTrainRows, g.nk - k_first);
+  const int64_t row = g.k0 + k_first;
+  join_sums<T, DH>(p0, step, parts, rows, a.scale, a.dk.p + row * a.dk.row + hk * a.dk.head, a.dk.row, left, tid);
+  join_sums<T, DH>(p0 + kTrainRows * DH, step, parts, rows, 1.f, a.dv.p + row * a.dv.row + hk * a.dv.head, a.dv.row,
+                   left, tid);
 }
 
 template <class T, int DH, bool REL>
@@ -292,8 +283,8 @@ hipError_t dkv_launch(const TrainArgs& a, int32_t n_units, hipStream_t s) {
   return hipGetLastError();
 }
 template <class T, int DH>
-hipError_t dkv_merge(const TrainArgs& a, int32_t n_units, hipStream_t s) {
-  train_dkv_merge_kernel<T, DH><<<dim3((unsigned)n_units * a.G), 256, 0, s>>>(a);
+hipError_t dkv_join(const TrainArgs& a, int32_t n_units, hipStream_t s) {
+  train_dkv_join_kernel<T, DH><<<dim3((unsigned)n_units * a.G), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -312,10 +303,10 @@ hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32
 #undef TX_CASE
 }
 
-hipError_t launch_train_dkv_merge(bool bf, int dh, const TrainArgs& a, int32_t n, hipStream_t s) {
+hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, int32_t n, hipStream_t s) {
   if (bf)
-    return dh == 32 ? dkv_merge<bf16, 32>(a, n, s) : dh == 64 ? dkv_merge<bf16, 64>(a, n, s) : dkv_merge<bf16, 128>(a, n, s);
-  return dh == 32 ? dkv_merge<float, 32>(a, n, s) : dh == 64 ? dkv_merge<float, 64>(a, n, s) : dkv_merge<float, 128>(a, n, s);
+    return dh == 32 ? dkv_join<bf16, 32>(a, n, s) : dh == 64 ? dkv_join<bf16, 64>(a, n, s) : dkv_join<bf16, 128>(a, n, s);
+  return dh == 32 ? dkv_join<float, 32>(a, n, s) : dh == 64 ? dkv_join<float, 64>(a, n, s) : dkv_join<float, 128>(a, n, s);
 }
 
 }  // namespace tx

@@ -58,7 +58,7 @@ __device__ __forceinline__ float diagonal_sums(const floatx16& x) {
 }
 
 template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4) void train_dq_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = dq_tile_bytes<T, DH>();
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
   const int local = unit - g.unit_q, part = local % parts;
-  const int qb = REL ? blocks - 1 - local / parts : local / parts;
+  const int qb = blocks - 1 - local / parts;
   const int q_first = qb * kTrainRows;
   const int hk = h / (a.H / a.G);
   const int R = REL ? a.R : 0, R1 = max(R, 1) - 1, entries = bias_entries(R);
@@ -258,37 +258,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void train_dq_kernel(c
 }
 
 template <class T, int DH>
-__global__ __launch_bounds__(256) void train_dq_merge_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256) void train_dq_join_kernel(const TrainArgs a) {
+  __shared__ __align__(16) char left[256 * 16];
   const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H, tid = threadIdx.x;
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
-  const int parts = g.parts_q, local = unit - g.unit_q;
+  const int parts = g.parts_q, local = unit - g.unit_q, qb = local / parts, q_first = qb * kTrainRows;
   if (parts == 1 || local % parts) return;
-  const int qb = local / parts, rows = min(kTrainRows, g.nq - qb * kTrainRows);
-  constexpr size_t SLOT = (size_t)kTrainRows * DH;
-  const float* const p0 = a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * SLOT;
-  constexpr int LPR = DH / 4;
-  for (int i = tid; i < rows * LPR; i += 256) {
-    const int r = i / LPR, f = i % LPR * 4;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-      const floatx4 x = *reinterpret_cast<const floatx4*>(p0 + p * SLOT * a.H + (size_t)r * DH + f);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] += x[t];
-    }
-    T* const out = (T*)(a.dq.p + (int64_t)(g.q0 + qb * kTrainRows + r) * a.dq.row + h * a.dq.head) + f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * a.scale);
-  }
+  join_sums<T, DH>(a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * (kTrainRows * DH),
+                   (size_t)a.H * kTrainRows * DH, parts, min(kTrainRows, g.nq - q_first), a.scale,
+                   a.dq.p + (int64_t)(g.q0 + q_first) * a.dq.row + h * a.dq.head, a.dq.row, (lds_char*)left, tid);
 }
 
-// Sums of 64 units' bucket sums (the first pass) ...
+// Sums of 32 units' bucket sums (the first pass) ...
+constexpr int kDrelChunk = 32;
 __global__ __launch_bounds__(256) void drel_chunk_kernel(const float* __restrict__ part, int n_units, int HR,
                                                          float* __restrict__ out) {
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i >= HR) return;
-  const int u0 = blockIdx.y * 64, u1 = min(u0 + 64, n_units);
-  float x = 0.f;
-  for (int u = u0; u < u1; ++u) x += part[(size_t)u * HR + i];
+  const int u0 = blockIdx.y * kDrelChunk, n = min(kDrelChunk, n_units - u0);
+  float v[kDrelChunk], x = 0.f;
+#pragma unroll
+  for (int u = 0; u < kDrelChunk; ++u) v[u] = u < n ? part[(size_t)(u0 + u) * HR + i] : 0.f;
+#pragma unroll
+  for (int u = 0; u < kDrelChunk; ++u) x += v[u];
   out[(size_t)blockIdx.y * HR + i] = x;
 }
 // ... and of all chunks, the last bucket as minus the others: a block per head.
@@ -300,6 +292,7 @@ __global__ __launch_bounds__(256) void drel_head_kernel(const float* __restrict_
   float others = 0.f;
   for (int b = tid; b < R - 1; b += 256) {
     float x = 0.f;
+#pragma unroll 16
     for (int c = 0; c < n; ++c) x += part[((size_t)c * H + h) * R + b];
     drel[(size_t)h * R + b] = (T)x;
     others += x;
@@ -322,8 +315,8 @@ hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 template <class T, int DH>
-hipError_t dq_merge(const TrainArgs& a, hipStream_t s) {
-  train_dq_merge_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
+hipError_t dq_join(const TrainArgs& a, hipStream_t s) {
+  train_dq_join_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -342,17 +335,18 @@ hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStr
 #undef TX_CASE
 }
 
-hipError_t launch_train_dq_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
-  if (bf) return dh == 32 ? dq_merge<bf16, 32>(a, s) : dh == 64 ? dq_merge<bf16, 64>(a, s) : dq_merge<bf16, 128>(a, s);
-  return dh == 32 ? dq_merge<float, 32>(a, s) : dh == 64 ? dq_merge<float, 64>(a, s) : dq_merge<float, 128>(a, s);
+hipError_t launch_train_dq_join(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
+  if (bf)
+    return dh == 32 ? dq_join<bf16, 32>(a, s) : dh == 64 ? dq_join<bf16, 64>(a, s) : dq_join<bf16, 128>(a, s);
+  return dh == 32 ? dq_join<float, 32>(a, s) : dh == 64 ? dq_join<float, 64>(a, s) : dq_join<float, 128>(a, s);
 }
 
 hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s) {
   const int HR = a.H * a.R;
   const float* part = a.drel_part;
   int n = a.R > 1 ? a.n_units : 0;
-  if (n > 64) {
-    const int chunks = (n + 63) / 64;
+  if (n > kDrelChunk) {
+    const int chunks = (n + kDrelChunk - 1) / kDrelChunk;
     drel_chunk_kernel<<<dim3((HR + 255) / 256, chunks), 256, 0, s>>>(part, n, HR, scratch);
     part = scratch, n = chunks;
   }

@@ -11,6 +11,11 @@ namespace {
 template <class T>
 constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
 
+// Blocks per CU: at d_head 64 and less four of 32 KB and 128 registers (98
+// against 103 us for 17 k queries of 2.3 k keys at 64; three no better than two).
+template <class T, int DH>
+constexpr int fwd_blocks() { return sizeof(T) == 2 && DH <= 64 ? 4 : 2; }
+
 template <class T, int DH>
 constexpr int fwd_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
 
@@ -20,7 +25,7 @@ constexpr int fwd_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
 // fragments read from the row-major tile (bf16: transposing LDS reads).
 // K and V are double-buffered, one barrier per tile.
 template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = fwd_tile_bytes<T, DH>();
@@ -32,8 +37,8 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
   const int local = unit - g.unit_q, part = local % parts;
-  // longest blocks of a causal group first
-  const int qb = REL ? blocks - 1 - local / parts : local / parts;
+  // a group's last rows see the most keys (later events have longer prefixes): first
+  const int qb = blocks - 1 - local / parts;
   const int q_first = qb * kTrainRows;
   const int hk = h / (a.H / a.G);
 
@@ -229,39 +234,62 @@ __global__ __launch_bounds__(256, 2) void train_fwd_kernel(const TrainArgs a) {
                       a.o.p + (int64_t)(g.q0 + q_wave) * a.o.row + h * a.o.head, a.o.row, n_rows, lane);
 }
 
-// Joins the parts of divided blocks: a block per (query block, head), 16 bytes of
-// output row per thread.
+// Joins the parts of a divided block of queries: with the parts' maxima m_p and
+// sums l_p, O = sum_p w_p O_p / sum_p w_p l_p, w_p = 2^(m_p - max m).
 template <class T, int DH>
-__global__ __launch_bounds__(256) void train_fwd_merge_kernel(const TrainArgs a) {
+__global__ __launch_bounds__(256) void train_fwd_join_kernel(const TrainArgs a) {
+  __shared__ __align__(16) char left_[256 * 20];
+  lds_char* const smem = (lds_char*)left_;
   const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H, tid = threadIdx.x;
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
-  const int parts = g.parts_q, local = unit - g.unit_q;
+  const int parts = g.parts_q, local = unit - g.unit_q, qb = local / parts;
   if (parts == 1 || local % parts) return;
-  const int qb = local / parts, rows = min(kTrainRows, g.nq - qb * kTrainRows);
   constexpr size_t SLOT = (size_t)kTrainRows * (DH + 2);
+  const int rows = min(kTrainRows, g.nq - qb * kTrainRows);
   const float* const p0 = a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * SLOT;
   const size_t step = SLOT * a.H;
-  constexpr int LPR = DH / 4;
-  for (int i = tid; i < rows * LPR; i += 256) {
-    const int r = i / LPR, f = i % LPR * 4;
-    float top = -INFINITY;
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, p0[p * step + kTrainRows * DH + r]);
-    float l = 0.f;
+  const Joiner<DH> j(rows, tid);
+  lds_floatx4* const left = (lds_floatx4*)smem;
+  lds_float* const left_l = (lds_float*)(smem + 256 * 16);
+  for (int r0 = 0; r0 < rows; r0 += j.at_once) {
+    const int r = r0 + j.slot;
+    float top = -INFINITY, l = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-      const float* s = p0 + p * step;
-      const float m = s[kTrainRows * DH + r];
-      const float wgt = m == -INFINITY ? (s[kTrainRows * (DH + 1) + r] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
-      if (wgt == 0.f) continue;
-      l += wgt * s[kTrainRows * (DH + 1) + r];
-      const floatx4 x = *reinterpret_cast<const floatx4*>(s + (size_t)r * DH + f);
+    if (r < rows) {
+#pragma unroll 8
+      for (int p = 0; p < parts; ++p) top = fmaxf(top, p0[p * step + kTrainRows * DH + r]);
+#pragma unroll 4
+      for (int p = j.share; p < parts; p += j.shares) {
+        const float* const s = p0 + p * step;
+        const float m = s[kTrainRows * DH + r], lp = s[kTrainRows * (DH + 1) + r];
+        const floatx4 x = *reinterpret_cast<const floatx4*>(s + (size_t)r * DH + j.f);
+        // a part without a visible key holds zeros and m = -inf (l says whether it is one: a
+        // part of nothing but NaN logits has that m too)
+        const float wgt = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        l += wgt * lp;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] += wgt * x[t];
+        for (int t = 0; t < 4; ++t) acc[t] += wgt * x[t];
+      }
     }
+    if (j.shares > 1) {
+      left[tid] = acc;
+      left_l[tid] = l;
+      __syncthreads();
+      for (int q = 1; q < j.shares && j.share == 0; ++q) {
+        const int from = tid + q * j.at_once * Joiner<DH>::LPR;
+        const floatx4 x = left[from];
+        l += left_l[from];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] += x[t];
+      }
+      __syncthreads();
+    }
+    if (r >= rows || j.share) continue;
     const int64_t row = g.q0 + qb * kTrainRows + r;
-    if (f == 0) a.lse[(int64_t)h * a.lse_ld + row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kTrainLn2;
+    if (j.f == 0)
+      a.lse[(int64_t)h * a.lse_ld + row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kTrainLn2;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* const out = (T*)(a.o.p + row * a.o.row + h * a.o.head) + f;
+    T* const out = (T*)(a.o.p + row * a.o.row + h * a.o.head) + j.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * inv);
   }
@@ -322,8 +350,8 @@ hipError_t fwd(const TrainArgs& a, hipStream_t s) {
 }
 
 template <class T, int DH>
-hipError_t fwd_merge(const TrainArgs& a, hipStream_t s) {
-  train_fwd_merge_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
+hipError_t fwd_join(const TrainArgs& a, hipStream_t s) {
+  train_fwd_join_kernel<T, DH><<<dim3((unsigned)a.n_units * a.H), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -342,9 +370,10 @@ hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipSt
 #undef TX_CASE
 }
 
-hipError_t launch_train_fwd_merge(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
-  if (bf) return dh == 32 ? fwd_merge<bf16, 32>(a, s) : dh == 64 ? fwd_merge<bf16, 64>(a, s) : fwd_merge<bf16, 128>(a, s);
-  return dh == 32 ? fwd_merge<float, 32>(a, s) : dh == 64 ? fwd_merge<float, 64>(a, s) : fwd_merge<float, 128>(a, s);
+hipError_t launch_train_fwd_join(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
+  if (bf)
+    return dh == 32 ? fwd_join<bf16, 32>(a, s) : dh == 64 ? fwd_join<bf16, 64>(a, s) : fwd_join<bf16, 128>(a, s);
+  return dh == 32 ? fwd_join<float, 32>(a, s) : dh == 64 ? fwd_join<float, 64>(a, s) : fwd_join<float, 128>(a, s);
 }
 
 hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
