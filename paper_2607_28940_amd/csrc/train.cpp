@@ -4,7 +4,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -23,10 +22,18 @@ using namespace tx;
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff - 4096;
-// Blocks that fill the card (256 CUs, two resident blocks each).
-constexpr int64_t kFullGrid = 512;
-constexpr int kMaxParts = 64;
-int kMinSteps = getenv("TXMIN") ? atoi(getenv("TXMIN")) : 4;  // EXPERIMENT
+// How a launch is cut into blocks (256 CUs). Narrow blocks below kWideGrid wide
+// ones: 1000 causal tokens of 8 heads (64 wide blocks) forward 48 -> 17 us, dq 50
+// -> 26, dk and dv 52 -> 25; 4096 (256) 100 -> 86, 127 -> 112, 149 -> 137; 17 k
+// queries of 2.3 k keys (1136) 98 -> 149.
+// Where that leaves fewer blocks than the card holds, the other side of a block
+// is divided into parts, towards kFullGrid blocks of an equal share, but none
+// below kMinSteps 64-row tiles (kMinStepsF32 in fp32, whose tiles take longer) a
+// wave, and not at all if that would not halve the block: what the parts write
+// and the join reads costs more than it saves (4096 tokens 86 -> 131 us towards
+// 1024 blocks, 1000 tokens 17 -> 31 us at 2 tiles a part).
+constexpr int64_t kWideGrid = 512, kFullGrid = 512;
+constexpr int kMaxParts = 64, kMinSteps = 4, kMinStepsF32 = 2;
 
 // Metadata goes up as kernel arguments, 3 KB a launch: no staging buffer whose
 // reuse would have to wait, and a captured graph keeps its own copy.
@@ -109,6 +116,7 @@ int check_rows(const tx_rows* t, const char* what, int es, int64_t heads, int dh
 struct AttnPlan {
   std::vector<TrainGroup> groups;
   std::vector<int32_t> ev_row, ev_prefix;  // event form
+  int q_rows = kWideRows, k_rows = kWideRows;
   int64_t units_q = 0, units_k = 0, tiles = 0, slots_q = 0, slots_k = 0;
   double pairs = 0;                        // visible (query, key) pairs
   int64_t rows_q = 0, rows_k = 0;          // rows of the call
@@ -122,20 +130,14 @@ struct AttnPlan {
   } at;
 };
 
-// Splits a side's blocks into parts over the other side's rows. A block of
-// steps tiles is worth dividing while the call as a whole would not fill the
-// card: the target is an equal share of all steps per resident block, but no
-// part below min_steps, where writing and joining partial results costs more
-// than it saves.
+// Parts of a block that goes through `steps` tiles.
 int parts_of(int64_t steps, int64_t total_steps, int min_steps) {
-  static int slots = getenv("TXSLOTS") ? atoi(getenv("TXSLOTS")) : 512;  // EXPERIMENT
-  static int pct = getenv("TXPCT") ? atoi(getenv("TXPCT")) : 200;  // EXPERIMENT
-  const int64_t target = std::max<int64_t>(min_steps, (total_steps + slots - 1) / slots);
-  if (steps * 100 < target * pct) return 1;
+  const int64_t target = std::max<int64_t>(min_steps, (total_steps + kFullGrid - 1) / kFullGrid);
+  if (steps < 2 * target) return 1;
   return (int)std::min<int64_t>(kMaxParts, (steps + target - 1) / target);
 }
 
-int64_t blocks_of(int64_t rows) { return (rows + kTrainRows - 1) / kTrainRows; }
+int64_t blocks_of(int64_t rows, int block = kWideRows) { return (rows + block - 1) / block; }
 int64_t tiles_of(int64_t rows) { return (rows + kTrainQTile - 1) / kTrainQTile; }
 
 void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) {
@@ -157,27 +159,36 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
     for (size_t i = 0; i < order.size(); ++i) sorted[i] = p.groups[order[i].second], keys[i] = reach(sorted[i]);
     p.groups.swap(sorted);
   }
+  // wide blocks where they would fill the card, narrow ones otherwise
+  int64_t wide_q = 0, wide_k = 0;
+  for (const TrainGroup& g : p.groups) wide_q += blocks_of(g.nq) * H, wide_k += blocks_of(g.nk) * G;
+  p.q_rows = wide_q >= kWideGrid ? kWideRows : kNarrowRows;
+  p.k_rows = wide_k >= kWideGrid ? kWideRows : kNarrowRows;
   int64_t steps_q = 0, steps_k = 0;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     const TrainGroup& g = p.groups[i];
     const double share = rel ? 0.5 : 1.0;  // a causal block covers half of the group's tiles on average
-    steps_q += (int64_t)std::ceil(blocks_of(g.nq) * tiles_of(keys[i]) * share) * H;
-    steps_k += (int64_t)std::ceil(blocks_of(g.nk) * tiles_of(g.nq) * share) * H;
+    steps_q += (int64_t)std::ceil(blocks_of(g.nq, p.q_rows) * tiles_of(keys[i]) * share) * H;
+    steps_k += (int64_t)std::ceil(blocks_of(g.nk, p.k_rows) * tiles_of(g.nq) * (H / G) * share) * G;
   }
+  const int min_steps = c.dtype == TX_F32 ? kMinStepsF32 : kMinSteps;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     TrainGroup& g = p.groups[i];
-    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, kMinSteps) : 1;
+    const int64_t bq = blocks_of(g.nq, p.q_rows), bk = blocks_of(g.nk, p.k_rows);
+    const int nq_steps = p.q_rows == kNarrowRows ? 4 * min_steps : min_steps,
+              nk_steps = p.k_rows == kNarrowRows ? 4 * min_steps : min_steps;
+    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, nq_steps) : 1;
     g.unit_q = (int32_t)p.units_q;
     g.slot_q = (int32_t)p.slots_q;
     g.qt0 = (int32_t)p.tiles;
-    p.units_q += blocks_of(g.nq) * g.parts_q;
-    if (g.parts_q > 1) p.slots_q += blocks_of(g.nq) * g.parts_q * H;
+    p.units_q += bq * g.parts_q;
+    if (g.parts_q > 1) p.slots_q += bq * g.parts_q * H;
     p.tiles += tiles_of(g.nq);
-    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * (H / G), steps_k, kMinSteps) : 1;
+    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * (H / G), steps_k, nk_steps) : 1;
     g.unit_k = (int32_t)p.units_k;
     g.slot_k = (int32_t)p.slots_k;
-    p.units_k += blocks_of(g.nk) * g.parts_k;
-    if (g.parts_k > 1) p.slots_k += blocks_of(g.nk) * g.parts_k * G;
+    p.units_k += bk * g.parts_k;
+    if (g.parts_k > 1) p.slots_k += bk * g.parts_k * G;
   }
   auto put = [&](const void* src, size_t n) {
     const size_t o = align_up(p.meta.size(), 64);
@@ -198,8 +209,8 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   p.at.tile_lim = take(rel ? 0 : p.tiles * sizeof(TileLim));
   p.at.stat = take(backward ? (size_t)H * p.rows_q * 8 : 0);
   // dq and then dk, dv use the slots in turn
-  const size_t sq = p.slots_q * (backward ? train_dq_slot(dh) : train_fwd_slot(dh));
-  const size_t sk = backward ? p.slots_k * train_dkv_slot(dh) : 0;
+  const size_t sq = p.slots_q * (backward ? train_dq_slot(p.q_rows, dh) : train_fwd_slot(p.q_rows, dh));
+  const size_t sk = backward ? p.slots_k * train_dkv_slot(p.k_rows, dh) : 0;
   p.at.partial = take(std::max(sq, sk) * 4);
   const size_t HR = rel && backward ? (size_t)H * c.rel_pos_buckets : 0;
   p.at.drel = take(HR * p.units_q * 4);
@@ -320,6 +331,7 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   a.scale = c.scale > 0.f ? c.scale : (float)(1.0 / std::sqrt((double)dh));
   a.scale_log2 = (float)(a.scale * 1.4426950408889634);
   a.partial = (float*)(w + p.at.partial);
+  a.q_rows = p.q_rows, a.k_rows = p.k_rows;
   a.drel_part = (float*)(w + p.at.drel);
   if (!rel)
     TX_HIP(launch_train_limits(a.groups, a.n_groups, (int32_t)p.tiles, (const int32_t*)(w + p.o_row),

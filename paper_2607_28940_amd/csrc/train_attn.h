@@ -21,9 +21,8 @@ namespace tx {
 
 // A group of a call, rows counted from the start of the tensors. Units are the
 // blocks of work of a launch per head: for query-side launches (forward, dq)
-// the group owns units unit_q .. , parts_q per block of kTrainRows queries, for
-// the key-side launch (dk, dv) unit_k .. , parts_k per block of kTrainRows
-// keys. Groups whose blocks are divided (parts > 1) keep their partial results
+// the group owns units unit_q .. , parts_q per block of queries, for the
+// key-side launch (dk, dv) unit_k .. , parts_k per block of keys. Groups whose blocks are divided (parts > 1) keep their partial results
 // in slots from slot_q / slot_k on, which a second launch joins in the order of
 // the parts (joining them in the block that finishes last saves that launch,
 // but the fences write whole L2 caches back: one token against 4096 keys took
@@ -35,7 +34,13 @@ struct TrainGroup {
   int32_t unit_k, parts_k, slot_k, e0;
   int32_t e1, pad[3];
 };
-constexpr int kTrainRows = 128;   // queries (forward, dq) or keys (dk, dv) of a block: 4 waves of 32
+// Rows of a block: queries (forward, dq) or keys (dk, dv). Wide blocks give each of
+// their four waves 32 of 128 rows and share the tiles of the other side. Narrow
+// ones give all four the same 32 rows and every fourth tile, each wave with
+// buffers of its own and no barrier between tiles, and add up at the end: for
+// calls whose wide blocks would leave most of the card idle, each with a long
+// chain of tiles.
+constexpr int kWideRows = 128, kNarrowRows = 32;
 constexpr int kTrainQTile = 64;   // granularity of the per-tile key limits
 constexpr int kTrainMaxRel = 2048;
 
@@ -66,6 +71,7 @@ struct TrainArgs {
   int32_t q_base;
   float scale, scale_log2;
   float* partial;       // slots of divided blocks
+  int32_t q_rows, k_rows;   // rows of a query-side and of a key-side block
   float* drel_part;     // [unit][H][R] sums of dS by bucket
 };
 
@@ -83,9 +89,9 @@ hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32
                                hipStream_t s);
 
 // floats of one partial slot
-inline size_t train_fwd_slot(int dh) { return (size_t)kTrainRows * (dh + 2); }
-inline size_t train_dq_slot(int dh) { return (size_t)kTrainRows * dh; }
-inline size_t train_dkv_slot(int dh) { return (size_t)2 * kTrainRows * dh; }
+__host__ __device__ inline size_t train_fwd_slot(int rows, int dh) { return (size_t)rows * (dh + 2); }
+__host__ __device__ inline size_t train_dq_slot(int rows, int dh) { return (size_t)rows * dh; }
+__host__ __device__ inline size_t train_dkv_slot(int rows, int dh) { return (size_t)2 * rows * dh; }
 
 #ifdef __HIPCC__
 
@@ -372,16 +378,16 @@ struct Wave {
 // transposing LDS read wait for all loads in flight, the next tile's among
 // them. So nothing waits for them but tiles_ready().
 // HELD: the lane's offsets stay in registers; otherwise they are made anew for
-// every tile.
-template <class T, int DH, int ROWS, bool HELD = true>
+// every tile. WAVES = 1: the wave copies the tile alone (wave index 0).
+template <class T, int DH, int ROWS, bool HELD = true, int WAVES = 4>
 struct TileDma {
   using G = Geo<T, DH>;
-  static constexpr int PER = ROWS * G::RB / 4096;  // pieces of a wave
+  static constexpr int PER = ROWS * G::RB / (1024 * WAVES);  // pieces of a wave
   uint32_t off[HELD ? PER : 1];
   int wave, lane;
   uint32_t ldb;
   __device__ __forceinline__ uint32_t offset(int u, int l) const {
-    const int r = (wave + 4 * u) * (1024 / G::RB) + l / G::UPR, s = l % G::UPR;
+    const int r = (wave + WAVES * u) * (1024 / G::RB) + l / G::UPR, s = l % G::UPR;
     return (uint32_t)r * ldb + ((uint32_t)(s ^ G::swz(r)) << 4);
   }
   __device__ __forceinline__ TileDma(int wave_, int lane_, int64_t row_bytes)
@@ -394,7 +400,9 @@ struct TileDma {
   __device__ __forceinline__ void load(const char* first, int rows, lds_char* tile) const {
     const int n = min(rows, ROWS);
     const uint64_t at = (uint64_t)first;
-    const u32x4_t r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)(n - 1) * ldb + G::RB, 0x00020000u};
+    // (uniform() where the compiler does not see it)
+    const u32x4_t r = {(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)) & 0xffffu,
+                       (uint32_t)uniform((n - 1) * (int)ldb) + G::RB, 0x00020000u};
     const uint32_t to = uniform((int)(uint32_t)(uintptr_t)tile) + wave * 1024;
     int l = lane;
     if (!HELD) asm volatile("" : "+v"(l));  // not hoisted
@@ -402,7 +410,7 @@ struct TileDma {
     for (int u = 0; u < PER; ++u)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    :
-                   : "s"(to + u * 4096), "v"(HELD ? off[HELD ? u : 0] : offset(u, l)), "s"(r)
+                   : "s"(to + u * 1024 * WAVES), "v"(HELD ? off[HELD ? u : 0] : offset(u, l)), "s"(r)
                    : "m0", "memory");
   }
 };
@@ -424,6 +432,12 @@ __device__ __forceinline__ void load_row_frags(const char* row, bool exists, int
 #pragma unroll
     for (int c = 0; c < Geo<T, DH>::NC; ++c) f[c] = *reinterpret_cast<const u32x4_t*>(row + 32 * c + 16 * hi);
   }
+}
+
+// A wave's own copies have landed.
+__device__ __forceinline__ void tile_ready() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
 }
 
 // Waits for values loaded from memory: left to the compiler, the wait would sit
@@ -489,6 +503,22 @@ __device__ __forceinline__ void store_partial(const floatx16 (&acc)[Geo<T, DH>::
     }
 }
 
+// Four floats of an output row.
+template <class T>
+__device__ __forceinline__ void store4(T* to, floatx4 x, float mul) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x4 y;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] = (bf16)(x[t] * mul);
+    *reinterpret_cast<bf16x4*>(to) = y;
+  } else {
+    floatx4 y;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] = x[t] * mul;
+    *reinterpret_cast<floatx4*>(to) = y;
+  }
+}
+
 // How a block of 256 threads goes through `rows` partial rows of DH floats: DH /
 // 4 threads a row, as many rows at once as there are threads or rows, and what
 // threads are left over on shares of the parts.
@@ -533,11 +563,52 @@ __device__ __forceinline__ void join_sums(const float* p0, size_t step, int part
       }
       __syncthreads();
     }
-    if (r < rows && j.share == 0) {
-      T* const to = (T*)(out + r * row_bytes) + j.f;
+    if (r < rows && j.share == 0) store4((T*)(out + r * row_bytes) + j.f, acc, mul);
+  }
+}
+
+// Narrow blocks: a wave parks its accumulator (columns = 32 rows of the output)
+// as fp32 rows in LDS, 16-byte unit u of row r at u ^ r within units of 8 or 16.
+template <int DH>
+struct Park {
+  static constexpr int UNITS = DH / 4, MASK = UNITS >= 16 ? 15 : 7;
+  static constexpr int BYTES = 32 * DH * 4;
+  static __device__ __forceinline__ lds_floatx4* at(lds_char* to, int r, int u) {
+    return (lds_floatx4*)(to + (r * UNITS + (u ^ (r & MASK))) * 16);
+  }
+  template <int NB>
+  static __device__ __forceinline__ void put(const floatx16 (&acc)[NB], lds_char* to, int lane) {
+    const int l32 = lane & 31, hi = lane >> 5;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) to[t] = (T)(acc[t] * mul);
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int gq = 0; gq < 4; ++gq) {
+        floatx4 x;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[t] = acc[db][4 * gq + t];
+        *at(to, l32, 8 * db + 2 * gq + hi) = x;
+      }
+  }
+};
+// The sum of the four waves' parked accumulators, row by row: into the output
+// (slot null) or a partial slot. `step` bytes between the waves' areas.
+template <class T, int DH>
+__device__ __forceinline__ void add_parked(lds_char* area, int step, float* slot, float mul, char* out,
+                                           int64_t row_bytes, int rows, int tid) {
+  using P = Park<DH>;
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) {
+    const int r = (tid + 256 * i) / P::UNITS, u = (tid + 256 * i) % P::UNITS;
+    floatx4 x = *P::at(area, r, u);
+#pragma unroll
+    for (int wv = 1; wv < 4; ++wv) {
+      const floatx4 y = *P::at(area + wv * step, r, u);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[t] += y[t];
     }
+    if (r >= rows) continue;
+    if (slot) *reinterpret_cast<floatx4*>(slot + r * DH + 4 * u) = x;
+    else store4((T*)(out + r * row_bytes) + 4 * u, x, mul);
   }
 }
 
@@ -553,6 +624,12 @@ __device__ __forceinline__ float bias_value(const T* __restrict__ rel, int R, in
 template <class T>
 __device__ __forceinline__ void stage_bias(lds_float* tab, const T* __restrict__ rel, int R, int h, int tid) {
   for (int i = tid; i < bias_entries(R); i += 256) tab[i] = bias_value(rel, R, h, i - kBiasPad);
+}
+
+// Lets a kernel use more than 64 KB of LDS a block.
+inline hipError_t allow_lds(const void* kernel, size_t bytes) {
+  return bytes <= 65536 ? hipSuccess
+                        : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
 #endif  // __HIPCC__

@@ -8,23 +8,35 @@
 namespace tx {
 namespace {
 
-// Rows of a query tile, and whether the block's V rows stay in LDS instead of
-// registers: at d_head 128 the accumulators of dk and dv (128 registers), the K
-// and V fragments (64) and a tile's S and dP do not fit 256 registers, and every
-// spill waits for the tiles in flight. In bf16, V in LDS with 32-row tiles keeps
-// two blocks on a CU (66 KB each): 17.8 -> 4.1 ms for 147 k queries of 2.3 k keys
-// on average. At d_head 64 V in LDS lets three blocks of 168 registers share a CU
-// (1.16 against 1.24 ms for 111 k queries of 2.3 k keys with two), at 32 it fits
-// registers four times over.
-template <class T, int DH>
-constexpr bool v_in_lds() { return sizeof(T) == 2 && DH >= 64; }
-template <class T, int DH>
-constexpr int query_tile() { return sizeof(T) == 2 && DH < 128 ? 64 : 32; }
-
-template <class T, int DH>
-constexpr int dkv_tile_bytes() { return query_tile<T, DH>() * Geo<T, DH>::RB; }
-template <class T, int DH>
-constexpr int dkv_lds_bytes() { return 4 * dkv_tile_bytes<T, DH>() + (v_in_lds<T, DH>() ? kTrainRows * Geo<T, DH>::RB : 0); }
+// Whether the block's V rows stay in LDS instead of registers: at d_head 128 the
+// accumulators of dk and dv (128 registers), the K and V fragments (64) and a
+// tile's S and dP do not fit 256 registers, and every spill waits for the tiles
+// in flight. In bf16, V in LDS with 32-row tiles keeps two blocks on a CU (66 KB
+// each): 17.8 -> 4.1 ms for 147 k queries of 2.3 k keys on average. At d_head 64
+// V in LDS lets three blocks of 168 registers share a CU (1.16 against 1.24 ms
+// for 111 k queries of 2.3 k keys with two), at 32 it fits registers four times
+// over. A narrow block has its CU to itself.
+template <class T, int DH, bool NARROW>
+constexpr bool v_in_lds() { return sizeof(T) == 2 && DH >= 64 && !NARROW; }
+// Rows of a query tile, tile buffers (Q and dO each) of a block or of a narrow
+// block's wave, bytes of a tile, and bytes of all tiles and V.
+template <class T, int DH, bool NARROW>
+constexpr int query_tile() { return sizeof(T) == 2 && DH < 128 && !NARROW ? 64 : 32; }
+template <class T, int DH, bool NARROW>
+constexpr int dkv_buffers() { return NARROW && sizeof(T) == 4 && DH == 128 ? 1 : 2; }
+template <class T, int DH, bool NARROW>
+constexpr int dkv_tile_bytes() { return query_tile<T, DH, NARROW>() * Geo<T, DH>::RB; }
+template <class T, int DH, bool NARROW>
+constexpr int dkv_lds_bytes() {
+  return (NARROW ? 4 : 1) * 2 * dkv_buffers<T, DH, NARROW>() * dkv_tile_bytes<T, DH, NARROW>() +
+         (v_in_lds<T, DH, NARROW>() ? kWideRows * Geo<T, DH>::RB : 0);
+}
+// Row statistics: [2 buffers][lse, D, limits][rows of a tile] of a block or of
+// each wave.
+template <class T, int DH, bool NARROW>
+constexpr int stat_floats() { return (NARROW ? 4 : 1) * 6 * query_tile<T, DH, NARROW>(); }
+template <class T, int DH, bool NARROW>
+constexpr int dkv_blocks() { return NARROW || sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4; }
 
 // A wave owns 32 keys, whose K (and V) fragments stay in registers. Per 32
 // queries: S = Q K^T and dP = dO V^T (lanes = keys), P and dS = P (dP - D),
@@ -32,21 +44,25 @@ constexpr int dkv_lds_bytes() { return 4 * dkv_tile_bytes<T, DH>() + (v_in_lds<T
 // accumulators and the columns of the dO and Q tiles read from LDS (bf16:
 // transposing reads). P and dS are rounded to bf16 for those products. Q, dO
 // and the rows' lse, D and key limits are double-buffered, one barrier a tile.
-template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4) void train_dkv_kernel(const TrainArgs a) {
+template <class T, int DH, bool REL, bool NARROW>
+__global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
-  constexpr int QT = query_tile<T, DH>(), QB = QT / 32, TB = dkv_tile_bytes<T, DH>();
+  constexpr int QT = query_tile<T, DH, NARROW>(), QB = QT / 32, TB = dkv_tile_bytes<T, DH, NARROW>();
+  constexpr int BUFS = dkv_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows, STEP = NARROW ? 4 : 1;
+  constexpr bool V_LDS = v_in_lds<T, DH, NARROW>();
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
-  lds_char* const sVb = smem + 4 * TB;                               // v_in_lds: the block's V rows
-  lds_float* const stat = (lds_float*)(smem + dkv_lds_bytes<T, DH>());  // [2 buffers][lse2, D, limits][QT]
-  lds_float* const tab = stat + 6 * QT;
+  lds_char* const sVb = smem + 2 * BUFS * TB;  // V_LDS: the block's V rows
+  lds_float* const stats = (lds_float*)(smem + dkv_lds_bytes<T, DH, NARROW>());
+  lds_float* const tab = stats + stat_floats<T, DH, NARROW>();
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int unit = blockIdx.x / a.G, hk = blockIdx.x % a.G, per = a.H / a.G;
   const TrainGroup g = a.groups[find_group<true>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_k, local = unit - g.unit_k, part = local % parts, kblk = local / parts;
-  const int k_first = kblk * kTrainRows, k_wave = k_first + wave * 32, key = k_wave + l32;
+  const int k_first = kblk * ROWS, k_wave = k_first + (NARROW ? 0 : wave * 32), key = k_wave + l32;
+  lds_char* const bufs = smem + (NARROW ? wave * 2 * BUFS * TB : 0);
+  lds_float* const stat = stats + (NARROW ? wave * 6 * QT : 0);
   const bool exists = key < g.nk;
   const int R = REL ? a.R : 0;
 
@@ -61,7 +77,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
     i1 = (int)((int64_t)n * (part + 1) / parts);
     i0 = (int)((int64_t)n * part / parts);
   }
-  const int R1 = max(R, 1) - 1, k_last = min(g.nk, k_first + kTrainRows) - 1;
+  const int R1 = max(R, 1) - 1, k_last = min(g.nk, k_first + ROWS) - 1;
   // causal tiles from t_far on have one bias, the last bucket's
   const int t_far = REL ? (k_last + R1 + QT - 1) / QT : 0;
   float far = 0.f;  // the head's last bucket
@@ -72,14 +88,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
     const TileLim x = a.tile_lim[g.qt0 + t];
     return x.hi <= k_first ? 0 : x.lo > k_last ? 2 : 1;
   };
-  const TileDma<T, DH, QT, !v_in_lds<T, DH>()> qd(wave, lane, a.q.row), dd(wave, lane, a.dO.row);
-  // The rows' statistics: threads 0 .. QT - 1 fetch lse and D, the next QT the
+  using Dma = TileDma<T, DH, QT, !V_LDS, NARROW ? 1 : 4>;
+  const Dma qd(NARROW ? 0 : wave, lane, a.q.row), dd(NARROW ? 0 : wave, lane, a.dO.row);
+  // The rows' statistics: threads (a narrow block's lanes) 0 .. QT - 1 fetch lse and D, the next QT the
   // limits, with the tile (rows past the last one read the last); they are parked
   // in LDS once the tile before has been computed, and nothing touches them till
   // then, as that would wait for the tile too.
   typedef float float2_t __attribute__((ext_vector_type(2)));
   auto fetch_stat = [&](int h, int t) {
-    int id = tid;
+    int id = NARROW ? lane : tid;
     asm volatile("" : "+v"(id));  // not hoisted
     const int64_t r = g.q0 + min(t * QT + id % QT, g.nq - 1) - a.q_base;
     const float2_t* p = (const float2_t*)a.row_stat + (h * a.stat_ld + r);
@@ -87,7 +104,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
     return *p;
   };
   auto park_stat = [&](float2_t x, int t, int b) {
-    int id = tid;
+    int id = NARROW ? lane : tid;
     asm volatile("" : "+v"(id));
     const int r = t * QT + id % QT;
     const bool ok = r < g.nq;
@@ -101,16 +118,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
   };
   auto fetch = [&](int h, int t, int b) {
     const int r = t * QT;
-    qd.load(a.q.p + (int64_t)(g.q0 + r) * a.q.row + h * a.q.head, g.nq - r, smem + b * TB);
-    dd.load(a.dO.p + (int64_t)(g.q0 + r) * a.dO.row + h * a.dO.head, g.nq - r, smem + (2 + b) * TB);
+    qd.load(a.q.p + (int64_t)(g.q0 + r) * a.q.row + h * a.q.head, g.nq - r, bufs + b * TB);
+    dd.load(a.dO.p + (int64_t)(g.q0 + r) * a.dO.row + h * a.dO.head, g.nq - r, bufs + (BUFS + b) * TB);
   };
   // One pass over the work list; STRICT: see train_fwd_kernel.
   auto pass = [&](auto strict_c) {
-    constexpr bool STRICT = decltype(strict_c)::value, V_LDS = v_in_lds<T, DH>();
+    constexpr bool STRICT = decltype(strict_c)::value;
     u32x4_t kf[Gm::NC], vf[V_LDS ? 1 : Gm::NC];
     load_row_frags<T, DH>(a.k.p + (int64_t)(g.k0 + key) * a.k.row + hk * a.k.head, exists, hi, kf);
     if constexpr (V_LDS) {
-      const TileDma<T, DH, kTrainRows, false> vd(wave, lane, a.v.row);
+      const TileDma<T, DH, kWideRows, false> vd(wave, lane, a.v.row);
       vd.load(a.v.p + (int64_t)(g.k0 + k_first) * a.v.row + hk * a.v.head, g.nk - k_first, sVb);
     } else {
       load_row_frags<T, DH>(a.v.p + (int64_t)(g.k0 + key) * a.v.row + hk * a.v.head, exists, hi, vf);
@@ -124,11 +141,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
     bool again = false;
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
-      const lds_char* const sQ = smem + b * TB;
-      const lds_char* const sO = smem + (2 + b) * TB;
+      const lds_char* const sQ = bufs + b * TB;
+      const lds_char* const sO = bufs + (BUFS + b) * TB;
       const lds_float* const ss = stat + b * 3 * QT;
       // at d_head 128 the fragments' addresses are cheaper made anew than held
-      int id = tid;
+      int id = NARROW ? lane : tid;
       if (V_LDS) asm volatile("" : "+v"(id));  // not hoisted
       const W w(id & 63);
 #pragma unroll
@@ -181,77 +198,126 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
         }
       }
     };
-    // The tiles t .. t1 - 1 of one class of one head, the next one on its way
-    // while one is computed. Ends on a barrier.
-    auto run = [&](auto masked_c, int h, int t, int t1) {
+    // The tiles of one class of the heads hh .. h1 - 1, the next one on its way
+    // while one is computed; a narrow block's wave takes every fourth of them, by
+    // itself. MANY: more heads than one may follow each other.
+    auto run = [&](auto masked_c, auto many_c, int hh, int h1) {
       constexpr int CLASS = decltype(masked_c)::value ? 1 : 2;
-      // the next tile of the class at or after t: causal ones by their index,
-      // event ones from a mask over 64 limit tiles that the wave looks at together
+      constexpr bool MANY = decltype(many_c)::value;
+      int t, t1;
+      // causal classes go by the tile's index, event ones by a mask over 64 limit
+      // tiles that the wave looks at together
       int m0 = -64;
       uint64_t mask = 0;
-      auto next = [&](int t) {
-        if (REL) {
-          while (t < t1 && tile_class(t) != CLASS) ++t;
-          return t;
-        }
-        while (t < t1) {
-          const int lt = t * QT / kTrainQTile;
-          if (lt >= m0 + 64) {
-            m0 = lt;
-            mask = __ballot((lt + lane) * kTrainQTile < g.nq && limit_class(lt + lane) == CLASS);
-          }
-          const uint64_t rest = mask >> (lt - m0);
-          if (rest & 1) break;
-          t = (rest ? lt + __builtin_ctzll(rest) : m0 + 64) * (kTrainQTile / QT);
-        }
-        return min(t, t1);
+      auto head = [&] {  // the head's share of the work list
+        t = t0 + max(0, i0 - hh * per_head);
+        t1 = t0 + min(per_head, i1 - hh * per_head);
+        if (REL && CLASS == 2) t = max(t, t_far);
+        if (NARROW) t += wave;
+        m0 = -64;
       };
-      t = next(t);
-      if (t >= t1) return;
-      fetch(h, t, 0);
-      park_stat(fetch_stat(h, t), t, 0);
-      for (int b = 0; t < t1; b ^= 1) {
-        tiles_ready();
-        const int tn = next(t + 1);
-        float2_t st = {0.f, 0.f};
-        if (tn < t1) {
-          fetch(h, tn, b ^ 1);
-          st = fetch_stat(h, tn);
+      auto seek = [&] {  // to the first tile of the class at or after t, in this head or a later one
+        for (;;) {
+          while (t < t1) {
+            if (REL) {
+              if (tile_class(t) == CLASS) return;
+              t += STEP;
+              continue;
+            }
+            const int lt = t * QT / kTrainQTile;
+            if (lt >= m0 + 64) {
+              m0 = lt;
+              mask = __ballot((lt + lane) * kTrainQTile < g.nq && limit_class(lt + lane) == CLASS);
+            }
+            const uint64_t rest = mask >> (lt - m0);
+            if (rest & 1) return;
+            if (NARROW) t += STEP;
+            else t = (rest ? lt + __builtin_ctzll(rest) : m0 + 64) * (kTrainQTile / QT);
+          }
+          if (!MANY || ++hh >= h1) return;
+          head();
         }
-        if (k_wave < g.nk) tile(masked_c, t, b);
-        if (tn < t1) park_stat(st, tn, b ^ 1);
-        t = tn;
+      };
+      head();
+      seek();
+      if (MANY ? hh >= h1 : t >= t1) return;
+      int h = hk * per + hh, now = t;
+      fetch(h, now, 0);
+      park_stat(fetch_stat(h, now), now, 0);
+      for (int b = 0;; b = BUFS == 2 ? b ^ 1 : 0) {
+        if (NARROW) tile_ready();
+        else tiles_ready();
+        t += STEP;
+        seek();
+        const bool more = MANY ? hh < h1 : t < t1;
+        if (MANY) h = hk * per + hh;
+        float2_t st = {0.f, 0.f};
+        if (more) {
+          if (BUFS == 2) fetch(h, t, b ^ 1);
+          st = fetch_stat(h, t);
+        }
+        if (k_wave < g.nk) tile(masked_c, now, b);
+        if (!more) break;
+        if (BUFS == 1) fetch(h, t, 0);
+        park_stat(st, t, BUFS == 2 ? b ^ 1 : 0);
+        now = t;
       }
-      __syncthreads();
+      if (!NARROW) __syncthreads();
     };
-    for (int hh = 0; hh < per; ++hh) {
-      const int ta = t0 + max(0, i0 - hh * per_head), tb = t0 + min(per_head, i1 - hh * per_head), h = hk * per + hh;
-      if (ta >= tb) continue;
-      if (REL) {
-        // (every wave is past the barrier that ended the head before)
-        stage_bias(tab, (const T*)a.rel, R, h, tid);
-        far = bias_value((const T*)a.rel, R, h, R1);
-      }
-      run(std::false_type{}, h, max(ta, t_far), tb);
-      run(std::true_type{}, h, ta, tb);
+    // a bias changes with the head; without one the heads follow each other
+    if (!REL && per > 1) {
+      run(std::false_type{}, std::true_type{}, 0, per);
+      run(std::true_type{}, std::true_type{}, 0, per);
+    } else if (!REL) {
+      run(std::false_type{}, std::false_type{}, 0, 1);
+      run(std::true_type{}, std::false_type{}, 0, 1);
     }
+    for (int hh = 0; REL && hh < per; ++hh) {
+      if (i0 >= (hh + 1) * per_head || i1 <= hh * per_head) continue;
+      const int h = hk * per + hh;
+      // (wide: every wave is past the barrier that ended the head before, and the
+      // first tile waits at one)
+      if (NARROW) __syncthreads();
+      stage_bias(tab, (const T*)a.rel, R, h, tid);
+      if (NARROW) __syncthreads();
+      far = bias_value((const T*)a.rel, R, h, R1);
+      run(std::false_type{}, std::false_type{}, hh, hh + 1);
+      run(std::true_type{}, std::false_type{}, hh, hh + 1);
+    }
+    if (V_LDS) tile_ready();  // (no tile may have waited for V)
     return again;
   };
   if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
-  if (parts > 1) {
-    float* const slot =
-        a.partial + ((size_t)g.slot_k + (size_t)((kblk * parts + part) * a.G + hk)) * (2 * kTrainRows * DH);
+  const int64_t first_row = g.k0 + k_first;
+  char* const dk_out = a.dk.p + first_row * a.dk.row + hk * a.dk.head;
+  char* const dv_out = a.dv.p + first_row * a.dv.row + hk * a.dv.head;
+  float* const slot = parts == 1 ? nullptr
+                                 : a.partial + ((size_t)g.slot_k + (size_t)((kblk * parts + part) * a.G + hk)) *
+                                                   train_dkv_slot(ROWS, DH);
+  if constexpr (NARROW) {
+    __syncthreads();  // every wave has done its tiles
+    Park<DH>::put(dk, bufs, lane);
+    __syncthreads();
+    add_parked<T, DH>(smem, 2 * BUFS * TB, slot, a.scale, dk_out, a.dk.row, g.nk - k_first, tid);
+    __syncthreads();
+    Park<DH>::put(dv, bufs, lane);
+    __syncthreads();
+    add_parked<T, DH>(smem, 2 * BUFS * TB, slot ? slot + ROWS * DH : nullptr, 1.f, dv_out, a.dv.row, g.nk - k_first, tid);
+    return;
+  }
+  if (slot) {
     const size_t r = wave * 32 + l32;
-    store_partial<T, DH>(dk, slot + r * DH, hi);
-    store_partial<T, DH>(dv, slot + (kTrainRows + r) * DH, hi);
+    if (exists) {
+      store_partial<T, DH>(dk, slot + r * DH, hi);
+      store_partial<T, DH>(dv, slot + (ROWS + r) * DH, hi);
+    }
     return;
   }
   if (k_wave >= g.nk) return;
-  const int64_t row = g.k0 + k_wave;
   lds_char* const stage = smem + wave * 32 * Gm::RB;
-  store_rows<T, DH>(dk, a.scale, stage, a.dk.p + row * a.dk.row + hk * a.dk.head, a.dk.row, g.nk - k_wave, lane);
+  store_rows<T, DH>(dk, a.scale, stage, dk_out + wave * 32 * a.dk.row, a.dk.row, g.nk - k_wave, lane);
   __builtin_amdgcn_wave_barrier();
-  store_rows<T, DH>(dv, 1.f, stage, a.dv.p + row * a.dv.row + hk * a.dv.head, a.dv.row, g.nk - k_wave, lane);
+  store_rows<T, DH>(dv, 1.f, stage, dv_out + wave * 32 * a.dv.row, a.dv.row, g.nk - k_wave, lane);
 }
 
 template <class T, int DH>
@@ -260,26 +326,25 @@ __global__ __launch_bounds__(256) void train_dkv_join_kernel(const TrainArgs a) 
   lds_char* const left = (lds_char*)left_;
   const int unit = blockIdx.x / a.G, hk = blockIdx.x % a.G, tid = threadIdx.x;
   const TrainGroup g = a.groups[find_group<true>(a.groups, a.n_groups, unit, tid & 63)];
-  const int parts = g.parts_k, local = unit - g.unit_k, kblk = local / parts, k_first = kblk * kTrainRows;
+  const int parts = g.parts_k, local = unit - g.unit_k, ROWS = a.k_rows, kblk = local / parts,
+            k_first = kblk * ROWS;
   if (parts == 1 || local % parts) return;
-  const float* const p0 = a.partial + ((size_t)g.slot_k + (size_t)(kblk * parts * a.G + hk)) * (2 * kTrainRows * DH);
-  const size_t step = (size_t)a.G * 2 * kTrainRows * DH;
-  const int rows = min(kTrainRows, g.nk - k_first);
+  const size_t slot = train_dkv_slot(ROWS, DH), step = (size_t)a.G * slot;
+  const float* const p0 = a.partial + ((size_t)g.slot_k + (size_t)(kblk * parts * a.G + hk)) * slot;
+  const int rows = min(ROWS, g.nk - k_first);
   const int64_t row = g.k0 + k_first;
   join_sums<T, DH>(p0, step, parts, rows, a.scale, a.dk.p + row * a.dk.row + hk * a.dk.head, a.dk.row, left, tid);
-  join_sums<T, DH>(p0 + kTrainRows * DH, step, parts, rows, 1.f, a.dv.p + row * a.dv.row + hk * a.dv.head, a.dv.row,
+  join_sums<T, DH>(p0 + ROWS * DH, step, parts, rows, 1.f, a.dv.p + row * a.dv.row + hk * a.dv.head, a.dv.row,
                    left, tid);
 }
 
-template <class T, int DH, bool REL>
+template <class T, int DH, bool REL, bool NARROW>
 hipError_t dkv_launch(const TrainArgs& a, int32_t n_units, hipStream_t s) {
-  const size_t lds = dkv_lds_bytes<T, DH>() + 6 * 4 * query_tile<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void*)train_dkv_kernel<T, DH, REL>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  train_dkv_kernel<T, DH, REL><<<dim3((unsigned)n_units * a.G), 256, lds, s>>>(a);
+  const size_t lds = dkv_lds_bytes<T, DH, NARROW>() + 4 * stat_floats<T, DH, NARROW>() +
+                     (REL ? 4 * (size_t)bias_entries(a.R) : 0);
+  const hipError_t e = allow_lds((const void*)train_dkv_kernel<T, DH, REL, NARROW>, lds);
+  if (e != hipSuccess) return e;
+  train_dkv_kernel<T, DH, REL, NARROW><<<dim3((unsigned)n_units * a.G), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 template <class T, int DH>
@@ -291,7 +356,10 @@ hipError_t dkv_join(const TrainArgs& a, int32_t n_units, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32_t n, hipStream_t s) {
-#define TX_CASE(T, D) return rel ? dkv_launch<T, D, true>(a, n, s) : dkv_launch<T, D, false>(a, n, s)
+  const bool narrow = a.k_rows == kNarrowRows;
+#define TX_CASE(T, D)                                                                                       \
+  return narrow ? (rel ? dkv_launch<T, D, true, true>(a, n, s) : dkv_launch<T, D, false, true>(a, n, s))    \
+                : (rel ? dkv_launch<T, D, true, false>(a, n, s) : dkv_launch<T, D, false, false>(a, n, s))
   if (bf) {
     if (dh == 32) TX_CASE(bf16, 32);
     if (dh == 64) TX_CASE(bf16, 64);

@@ -14,11 +14,19 @@
 namespace tx {
 namespace {
 
-template <class T>
-constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
-
-template <class T, int DH>
-constexpr int dq_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
+// As in the forward.
+template <class T, bool NARROW>
+constexpr int key_tile() { return sizeof(T) == 2 && !NARROW ? 64 : 32; }
+template <class T, int DH, bool NARROW>
+constexpr int dq_buffers() { return NARROW && sizeof(T) == 4 && DH == 128 ? 1 : 2; }
+template <class T, int DH, bool NARROW>
+constexpr int dq_tile_bytes() { return key_tile<T, NARROW>() * Geo<T, DH>::RB; }
+template <class T, int DH, bool NARROW>
+constexpr int dq_lds_bytes() {
+  return (NARROW ? 4 : 1) * 2 * dq_buffers<T, DH, NARROW>() * dq_tile_bytes<T, DH, NARROW>();
+}
+template <class T, int DH, bool NARROW>
+constexpr int dq_blocks() { return NARROW || sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4; }
 
 // Per wave and 32 keys: S^T = K Q^T, dP^T = V dO^T (lanes = queries, so lse and
 // D are one register each), dS = P (dP - D), dQ^T += K^T dS^T with dS^T taken
@@ -57,21 +65,22 @@ __device__ __forceinline__ float diagonal_sums(const floatx16& x) {
   return sum;
 }
 
-template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4) void train_dq_kernel(const TrainArgs a) {
+template <class T, int DH, bool REL, bool NARROW>
+__global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
-  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = dq_tile_bytes<T, DH>();
+  constexpr int KT = key_tile<T, NARROW>(), KB = KT / 32, TB = dq_tile_bytes<T, DH, NARROW>();
+  constexpr int BUFS = dq_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows;
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
-  lds_float* const tab = (lds_float*)(smem + 4 * TB);
+  lds_float* const tab = (lds_float*)(smem + dq_lds_bytes<T, DH, NARROW>());
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
-  const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
+  const int parts = g.parts_q, blocks = (g.nq + ROWS - 1) / ROWS;
   const int local = unit - g.unit_q, part = local % parts;
   const int qb = blocks - 1 - local / parts;
-  const int q_first = qb * kTrainRows;
+  const int q_first = qb * ROWS;
   const int hk = h / (a.H / a.G);
   const int R = REL ? a.R : 0, R1 = max(R, 1) - 1, entries = bias_entries(R);
   const bool sums = REL && R > 1;
@@ -79,11 +88,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
 
   int k_end;
   if (REL) {
-    k_end = min(g.nq, q_first + kTrainRows);
+    k_end = min(g.nq, q_first + ROWS);
   } else {
-    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     k_end = tl[0].hi;
-    if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+    if (!NARROW && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
   const float far = REL ? bias_value((const T*)a.rel, R, h, R1) : 0.f;
@@ -94,9 +103,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
   if (REL) {
     t_plain = fabsf(far) < 0x1p20f ? max(0, q_first - R1 + 1) / KT : 0;
   } else {
-    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     t_plain = tl[0].lo;
-    if (q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    if (!NARROW && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
     t_plain /= KT;
   }
   if (parts > 1) {
@@ -106,7 +115,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
   }
   t_plain = min(t_plain, t_end);
 
-  const int q_wave = q_first + wave * 32, q_row = q_wave + l32;
+  const int q_wave = q_first + (NARROW ? 0 : wave * 32), q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
   const int64_t row = g.q0 + q_row;
   float D = 0.f;
@@ -132,7 +141,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
   if (exists) {
     const float x = a.lse[(int64_t)h * a.lse_ld + row];
     if (x != -INFINITY) lse2 = x * kTrainLog2e;
-    if (part == 0 && hi == 0) {
+    if (part == 0 && hi == 0 && (!NARROW || wave == 0)) {
       float* const st = a.row_stat + 2 * ((int64_t)h * a.stat_ld + row - a.q_base);
       st[0] = lse2;
       st[1] = D;
@@ -153,13 +162,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
   floatx16 dq[Gm::NB];
 
   const W w(lane);
-  const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
+  using Dma = TileDma<T, DH, KT, true, NARROW ? 1 : 4>;
+  const Dma kd(NARROW ? 0 : wave, lane, a.k.row), vd(NARROW ? 0 : wave, lane, a.v.row);
+  lds_char* const bufs = smem + (NARROW ? wave * 2 * BUFS * TB : 0);
   const char* const kp = a.k.p + (int64_t)g.k0 * a.k.row + hk * a.k.head;
   const char* const vp = a.v.p + (int64_t)g.k0 * a.v.row + hk * a.v.head;
   auto fetch = [&](int t, int b) {
     const int r = t * KT;
-    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
-    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
+    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, bufs + b * TB);
+    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, bufs + (BUFS + b) * TB);
   };
   // One pass over the keys; STRICT: see train_fwd_kernel.
   auto pass = [&](auto strict_c) {
@@ -177,8 +188,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
       const int k0 = t * KT;
-      const lds_char* const sK = smem + b * TB;
-      const lds_char* const sV = smem + (2 + b) * TB;
+      const lds_char* const sK = bufs + b * TB;
+      const lds_char* const sV = bufs + (BUFS + b) * TB;
       const int d0 = min(q_row - k0, R1 + kBiasPad - 1) - 4 * hi + kBiasPad;
       const float off = far - lse2;
 #pragma unroll
@@ -216,23 +227,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
         }
       }
     };
-    if (t_begin < t_end) fetch(t_begin, 0);
+    // a wide block's waves go through the tiles together, a narrow one's through
+    // every fourth, each at its own pace
+    constexpr int STEP = NARROW ? 4 : 1;
+    auto ready = [&] {
+      if (NARROW) tile_ready();
+      else tiles_ready();
+    };
+    int t = t_begin + (NARROW ? wave : 0), b = 0;
+    auto run = [&](auto masked_c, int end, bool rows_here) {
+      for (; t < end; t += STEP) {
+        if (BUFS == 2 && t + STEP < t_end) fetch(t + STEP, b ^ 1);
+        if (decltype(masked_c)::value ? t * KT < lim_hi : rows_here) tile(masked_c, t, b);
+        if (BUFS == 1 && t + STEP < t_end) fetch(t + STEP, 0);
+        ready();
+        if (BUFS == 2) b ^= 1;
+      }
+    };
+    if (NARROW) __syncthreads();  // (the bias table and the sums)
+    if (t < t_end) fetch(t, 0);
     pin(qf), pin(df), pin(lim), pin(lse2), pin(D);
-    tiles_ready();
-    int t = t_begin;
-    const bool rows_here = q_wave < g.nq;
-    for (; t < t_plain; ++t) {
-      const int b = (t - t_begin) & 1;
-      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-      if (rows_here) tile(std::false_type{}, t, b);
-      tiles_ready();
-    }
-    for (; t < t_end; ++t) {
-      const int b = (t - t_begin) & 1;
-      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-      if (t * KT < lim_hi) tile(std::true_type{}, t, b);
-      tiles_ready();
-    }
+    ready();
+    run(std::false_type{}, t_plain, q_wave < g.nq);
+    run(std::true_type{}, t_end, true);
+    if (NARROW) __syncthreads();
     return again;
   };
   if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
@@ -247,14 +265,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 
       out[d] = x;
     }
   }
-  if (parts > 1) {
-    float* const slot = a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) * (kTrainRows * DH);
-    store_partial<T, DH>(dq, slot + (size_t)(wave * 32 + l32) * DH, hi);
+  float* const slot = parts == 1 ? nullptr
+                                 : a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) *
+                                                   train_dq_slot(ROWS, DH);
+  char* const out = a.dq.p + (int64_t)(g.q0 + q_first) * a.dq.row + h * a.dq.head;
+  if constexpr (NARROW) {
+    Park<DH>::put(dq, bufs, lane);
+    __syncthreads();
+    add_parked<T, DH>(smem, 2 * BUFS * TB, slot, a.scale, out, a.dq.row, g.nq - q_first, tid);
+    return;
+  }
+  if (slot) {
+    if (exists) store_partial<T, DH>(dq, slot + (size_t)(wave * 32 + l32) * DH, hi);
     return;
   }
   if (q_wave < g.nq)
-    store_rows<T, DH>(dq, a.scale, smem + wave * 32 * Gm::RB,
-                      a.dq.p + (int64_t)(g.q0 + q_wave) * a.dq.row + h * a.dq.head, a.dq.row, g.nq - q_wave, lane);
+    store_rows<T, DH>(dq, a.scale, smem + wave * 32 * Gm::RB, out + wave * 32 * a.dq.row, a.dq.row, g.nq - q_wave, lane);
 }
 
 template <class T, int DH>
@@ -262,10 +288,11 @@ __global__ __launch_bounds__(256) void train_dq_join_kernel(const TrainArgs a) {
   __shared__ __align__(16) char left[256 * 16];
   const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H, tid = threadIdx.x;
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
-  const int parts = g.parts_q, local = unit - g.unit_q, qb = local / parts, q_first = qb * kTrainRows;
+  const int parts = g.parts_q, local = unit - g.unit_q, qb = local / parts, q_first = qb * a.q_rows;
   if (parts == 1 || local % parts) return;
-  join_sums<T, DH>(a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * (kTrainRows * DH),
-                   (size_t)a.H * kTrainRows * DH, parts, min(kTrainRows, g.nq - q_first), a.scale,
+  const size_t slot = train_dq_slot(a.q_rows, DH);
+  join_sums<T, DH>(a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * slot, (size_t)a.H * slot, parts,
+                   min(a.q_rows, g.nq - q_first), a.scale,
                    a.dq.p + (int64_t)(g.q0 + q_first) * a.dq.row + h * a.dq.head, a.dq.row, (lds_char*)left, tid);
 }
 
@@ -303,15 +330,13 @@ __global__ __launch_bounds__(256) void drel_head_kernel(const float* __restrict_
   if (tid == 0) drel[(size_t)h * R + R - 1] = (T)(0.f - (wsum[0] + wsum[1] + wsum[2] + wsum[3]));
 }
 
-template <class T, int DH, bool REL>
+template <class T, int DH, bool REL, bool NARROW>
 hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
-  const size_t lds = 4 * dq_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 5 : 1) : 0);
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void*)train_dq_kernel<T, DH, REL>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  train_dq_kernel<T, DH, REL><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  const size_t lds =
+      dq_lds_bytes<T, DH, NARROW>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 5 : 1) : 0);
+  const hipError_t e = allow_lds((const void*)train_dq_kernel<T, DH, REL, NARROW>, lds);
+  if (e != hipSuccess) return e;
+  train_dq_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 template <class T, int DH>
@@ -323,7 +348,10 @@ hipError_t dq_join(const TrainArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
-#define TX_CASE(T, D) return rel ? dq_launch<T, D, true>(a, s) : dq_launch<T, D, false>(a, s)
+  const bool narrow = a.q_rows == kNarrowRows;
+#define TX_CASE(T, D)                                                                               \
+  return narrow ? (rel ? dq_launch<T, D, true, true>(a, s) : dq_launch<T, D, false, true>(a, s))    \
+                : (rel ? dq_launch<T, D, true, false>(a, s) : dq_launch<T, D, false, false>(a, s))
   if (bf) {
     if (dh == 32) TX_CASE(bf16, 32);
     if (dh == 64) TX_CASE(bf16, 64);

@@ -8,48 +8,55 @@
 namespace tx {
 namespace {
 
-template <class T>
-constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
-
-// Blocks per CU: at d_head 64 and less four of 32 KB and 128 registers (98
+// Keys of a tile, tile buffers (K and V each) of a block or of a narrow block's
+// wave, bytes of a tile, and bytes of all tiles.
+template <class T, bool NARROW>
+constexpr int key_tile() { return sizeof(T) == 2 && !NARROW ? 64 : 32; }
+template <class T, int DH, bool NARROW>
+constexpr int fwd_buffers() { return NARROW && sizeof(T) == 4 && DH == 128 ? 1 : 2; }
+template <class T, int DH, bool NARROW>
+constexpr int fwd_tile_bytes() { return key_tile<T, NARROW>() * Geo<T, DH>::RB; }
+template <class T, int DH, bool NARROW>
+constexpr int fwd_lds_bytes() {
+  return (NARROW ? 4 : 1) * 2 * fwd_buffers<T, DH, NARROW>() * fwd_tile_bytes<T, DH, NARROW>();
+}
+// Wide blocks per CU: at d_head 64 and less four of 32 KB and 128 registers (98
 // against 103 us for 17 k queries of 2.3 k keys at 64; three no better than two).
-template <class T, int DH>
-constexpr int fwd_blocks() { return sizeof(T) == 2 && DH <= 64 ? 4 : 2; }
-
-template <class T, int DH>
-constexpr int fwd_tile_bytes() { return key_tile<T>() * Geo<T, DH>::RB; }
+template <class T, int DH, bool NARROW>
+constexpr int fwd_blocks() { return NARROW ? 1 : sizeof(T) == 2 && DH <= 64 ? 4 : 2; }
 
 // Per wave and tile of KT keys: S^T = K Q^T with keys as rows, so a lane holds
 // KT / 2 keys of one query and the softmax needs one exchange with lane l ^ 32;
 // then O^T += V^T P^T, P^T taken from the accumulators as they are and V^T
 // fragments read from the row-major tile (bf16: transposing LDS reads).
 // K and V are double-buffered, one barrier per tile.
-template <class T, int DH, bool REL>
-__global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(const TrainArgs a) {
+template <class T, int DH, bool REL, bool NARROW>
+__global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
-  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = fwd_tile_bytes<T, DH>();
+  constexpr int KT = key_tile<T, NARROW>(), KB = KT / 32, TB = fwd_tile_bytes<T, DH, NARROW>();
+  constexpr int BUFS = fwd_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows;
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
-  lds_float* const tab = (lds_float*)(smem + 4 * TB);
+  lds_float* const tab = (lds_float*)(smem + fwd_lds_bytes<T, DH, NARROW>());
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
-  const int parts = g.parts_q, blocks = (g.nq + kTrainRows - 1) / kTrainRows;
+  const int parts = g.parts_q, blocks = (g.nq + ROWS - 1) / ROWS;
   const int local = unit - g.unit_q, part = local % parts;
   // a group's last rows see the most keys (later events have longer prefixes): first
   const int qb = blocks - 1 - local / parts;
-  const int q_first = qb * kTrainRows;
+  const int q_first = qb * ROWS;
   const int hk = h / (a.H / a.G);
 
   // keys that any row of the block sees, and the block's share of them
   int k_end;
   if (REL) {
-    k_end = min(g.nq, q_first + kTrainRows);
+    k_end = min(g.nq, q_first + ROWS);
   } else {
-    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     k_end = tl[0].hi;
-    if (q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+    if (!NARROW && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
   const int R = REL ? a.R : 0, R1 = max(R, 1) - 1;  // R1: the first distance of the last bucket
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
@@ -65,9 +72,9 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
   if (REL) {
     t_plain = fabsf(far) < 0x1p20f ? max(0, q_first - R1 + 1) / KT : 0;
   } else {
-    const TileLim* tl = a.tile_lim + g.qt0 + 2 * qb;
+    const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     t_plain = tl[0].lo;
-    if (q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    if (!NARROW && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
     t_plain /= KT;
   }
   if (parts > 1) {
@@ -77,7 +84,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
   }
   t_plain = min(t_plain, t_end);
 
-  const int q_wave = q_first + wave * 32;         // first query of the wave, within the group
+  const int q_wave = q_first + (NARROW ? 0 : wave * 32);  // first query of the wave, within the group
   const int q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
   int lim = 0;  // visible keys of the lane's query
@@ -96,13 +103,15 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
   float m, l;
 
   const W w(lane);
-  const TileDma<T, DH, KT> kd(wave, lane, a.k.row), vd(wave, lane, a.v.row);
+  using Dma = TileDma<T, DH, KT, true, NARROW ? 1 : 4>;
+  const Dma kd(NARROW ? 0 : wave, lane, a.k.row), vd(NARROW ? 0 : wave, lane, a.v.row);
+  lds_char* const bufs = smem + (NARROW ? wave * 2 * BUFS * TB : 0);
   const char* const kp = a.k.p + (int64_t)g.k0 * a.k.row + hk * a.k.head;
   const char* const vp = a.v.p + (int64_t)g.k0 * a.v.row + hk * a.v.head;
   auto fetch = [&](int t, int b) {
     const int r = t * KT;
-    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, smem + b * TB);
-    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, smem + (2 + b) * TB);
+    kd.load(kp + (int64_t)r * a.k.row, g.nk - r, bufs + b * TB);
+    vd.load(vp + (int64_t)r * a.v.row, g.nk - r, bufs + (BUFS + b) * TB);
   };
   // One pass over the keys. A masked tile whose values are not all finite has
   // to keep them from the pairs out of sight; that is rare, and its code would
@@ -123,8 +132,8 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
       const int k0 = t * KT;
-      const lds_char* const sK = smem + b * TB;
-      const lds_char* const sV = smem + (2 + b) * TB;
+      const lds_char* const sK = bufs + b * TB;
+      const lds_char* const sV = bufs + (BUFS + b) * TB;
       floatx16 s[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) w.rows_product(sK, kb, qf, s[kb]);
@@ -193,35 +202,83 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
         }
       }
     };
-    if (t_begin < t_end) fetch(t_begin, 0);
+    // a wide block's waves go through the tiles together, a narrow one's through
+    // every fourth, each at its own pace
+    constexpr int STEP = NARROW ? 4 : 1;
+    auto ready = [&] {
+      if (NARROW) tile_ready();
+      else tiles_ready();
+    };
+    int t = t_begin + (NARROW ? wave : 0), b = 0;
+    auto run = [&](auto masked_c, int end, bool rows_here) {
+      for (; t < end; t += STEP) {
+        if (BUFS == 2 && t + STEP < t_end) fetch(t + STEP, b ^ 1);
+        if (decltype(masked_c)::value ? t * KT < lim_hi : rows_here) tile(masked_c, t, b);
+        if (BUFS == 1 && t + STEP < t_end) fetch(t + STEP, 0);
+        ready();
+        if (BUFS == 2) b ^= 1;
+      }
+    };
+    if (NARROW) __syncthreads();  // (the bias table)
+    if (t < t_end) fetch(t, 0);
     pin(qf), pin(lim);
-    tiles_ready();
-    int t = t_begin;
-    const bool rows_here = q_wave < g.nq;
-    for (; t < t_plain; ++t) {
-      const int b = (t - t_begin) & 1;
-      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-      if (rows_here) tile(std::false_type{}, t, b);
-      tiles_ready();
-    }
-    for (; t < t_end; ++t) {
-      const int b = (t - t_begin) & 1;
-      if (t + 1 < t_end) fetch(t + 1, b ^ 1);
-      if (t * KT < lim_hi) tile(std::true_type{}, t, b);
-      tiles_ready();
-    }
+    ready();
+    run(std::false_type{}, t_plain, q_wave < g.nq);
+    run(std::true_type{}, t_end, true);
+    if (NARROW) __syncthreads();
     return again;
   };
   if (__syncthreads_or(pass(std::false_type{}))) (void)pass(std::true_type{});
   l = xor32_sum(l);
-  if (parts > 1) {
-    float* const slot =
-        a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) * (kTrainRows * (DH + 2));
+  const int64_t first_row = g.q0 + q_first;
+  char* const out = a.o.p + first_row * a.o.row + h * a.o.head;
+  float* const slot = parts == 1 ? nullptr
+                                 : a.partial + ((size_t)g.slot_q + (size_t)((qb * parts + part) * a.H + h)) *
+                                                   train_fwd_slot(ROWS, DH);
+  if constexpr (NARROW) {
+    // (the pass ended on a barrier: the tiles are free)
+    constexpr int STEP = 2 * BUFS * TB;
+    lds_float* const ml = (lds_float*)(bufs + Park<DH>::BYTES);
+    Park<DH>::put(o, bufs, lane);
+    if (hi == 0) ml[l32] = m, ml[32 + l32] = l;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) {
+      const int r = (tid + 256 * i) / Park<DH>::UNITS, u = (tid + 256 * i) % Park<DH>::UNITS;
+      if (q_first + r >= g.nq) continue;
+      float mw[4], lw[4], top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int wv = 0; wv < 4; ++wv) {
+        const lds_float* const x = (const lds_float*)(smem + wv * STEP + Park<DH>::BYTES);
+        mw[wv] = x[r], lw[wv] = x[32 + r];
+        top = fmaxf(top, mw[wv]);
+      }
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int wv = 0; wv < 4; ++wv) {
+        const float wgt = mw[wv] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw[wv] - top);  // (as in the join)
+        const floatx4 x = *Park<DH>::at(smem + wv * STEP, r, u);
+        sum += wgt * lw[wv];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] += wgt * x[t];
+      }
+      if (slot) {
+        *reinterpret_cast<floatx4*>(slot + r * DH + 4 * u) = acc;
+        if (u == 0) slot[ROWS * DH + r] = top, slot[ROWS * (DH + 1) + r] = sum;
+      } else {
+        store4((T*)(out + r * a.o.row) + 4 * u, acc, sum == 0.f ? 0.f : 1.f / sum);
+        if (u == 0)
+          a.lse[(int64_t)h * a.lse_ld + first_row + r] =
+              sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kTrainLn2;
+      }
+    }
+    return;
+  }
+  if (slot) {
     const int r = wave * 32 + l32;
-    store_partial<T, DH>(o, slot + (size_t)r * DH, hi);
-    if (hi == 0) {
-      slot[kTrainRows * DH + r] = m;
-      slot[kTrainRows * (DH + 1) + r] = l;
+    if (exists) {
+      store_partial<T, DH>(o, slot + (size_t)r * DH, hi);
+      if (hi == 0) slot[ROWS * DH + r] = m, slot[ROWS * (DH + 1) + r] = l;
     }
     return;
   }
@@ -230,8 +287,8 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH>())) void train_fwd_kernel(c
   if (exists && hi == 0)
     a.lse[(int64_t)h * a.lse_ld + g.q0 + q_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kTrainLn2;
   if (n_rows > 0)
-    store_rows<T, DH>(o, l == 0.f ? 0.f : 1.f / l, smem + wave * 32 * Gm::RB,
-                      a.o.p + (int64_t)(g.q0 + q_wave) * a.o.row + h * a.o.head, a.o.row, n_rows, lane);
+    store_rows<T, DH>(o, l == 0.f ? 0.f : 1.f / l, smem + wave * 32 * Gm::RB, out + wave * 32 * a.o.row, a.o.row, n_rows,
+                      lane);
 }
 
 // Joins the parts of a divided block of queries: with the parts' maxima m_p and
@@ -244,8 +301,8 @@ __global__ __launch_bounds__(256) void train_fwd_join_kernel(const TrainArgs a) 
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, tid & 63)];
   const int parts = g.parts_q, local = unit - g.unit_q, qb = local / parts;
   if (parts == 1 || local % parts) return;
-  constexpr size_t SLOT = (size_t)kTrainRows * (DH + 2);
-  const int rows = min(kTrainRows, g.nq - qb * kTrainRows);
+  const int ROWS = a.q_rows, rows = min(ROWS, g.nq - qb * ROWS);
+  const size_t SLOT = train_fwd_slot(ROWS, DH);
   const float* const p0 = a.partial + ((size_t)g.slot_q + (size_t)(qb * parts * a.H + h)) * SLOT;
   const size_t step = SLOT * a.H;
   const Joiner<DH> j(rows, tid);
@@ -257,11 +314,11 @@ __global__ __launch_bounds__(256) void train_fwd_join_kernel(const TrainArgs a) 
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     if (r < rows) {
 #pragma unroll 8
-      for (int p = 0; p < parts; ++p) top = fmaxf(top, p0[p * step + kTrainRows * DH + r]);
+      for (int p = 0; p < parts; ++p) top = fmaxf(top, p0[p * step + ROWS * DH + r]);
 #pragma unroll 4
       for (int p = j.share; p < parts; p += j.shares) {
         const float* const s = p0 + p * step;
-        const float m = s[kTrainRows * DH + r], lp = s[kTrainRows * (DH + 1) + r];
+        const float m = s[ROWS * DH + r], lp = s[ROWS * (DH + 1) + r];
         const floatx4 x = *reinterpret_cast<const floatx4*>(s + (size_t)r * DH + j.f);
         // a part without a visible key holds zeros and m = -inf (l says whether it is one: a
         // part of nothing but NaN logits has that m too)
@@ -285,13 +342,11 @@ __global__ __launch_bounds__(256) void train_fwd_join_kernel(const TrainArgs a) 
       __syncthreads();
     }
     if (r >= rows || j.share) continue;
-    const int64_t row = g.q0 + qb * kTrainRows + r;
+    const int64_t row = g.q0 + qb * ROWS + r;
     if (j.f == 0)
       a.lse[(int64_t)h * a.lse_ld + row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kTrainLn2;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* const out = (T*)(a.o.p + row * a.o.row + h * a.o.head) + j.f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) out[t] = (T)(acc[t] * inv);
+    store4((T*)(a.o.p + row * a.o.row + h * a.o.head) + j.f, acc, inv);
   }
 }
 
@@ -337,15 +392,12 @@ __global__ __launch_bounds__(64) void train_limits_kernel(const TrainGroup* __re
   if (lane == 0) tile_lim[tile] = TileLim{mn, mx};
 }
 
-template <class T, int DH, bool REL>
+template <class T, int DH, bool REL, bool NARROW>
 hipError_t fwd(const TrainArgs& a, hipStream_t s) {
-  const size_t lds = 4 * fwd_tile_bytes<T, DH>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void*)train_fwd_kernel<T, DH, REL>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  train_fwd_kernel<T, DH, REL><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  const size_t lds = fwd_lds_bytes<T, DH, NARROW>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
+  const hipError_t e = allow_lds((const void*)train_fwd_kernel<T, DH, REL, NARROW>, lds);
+  if (e != hipSuccess) return e;
+  train_fwd_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -358,7 +410,10 @@ hipError_t fwd_join(const TrainArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
-#define TX_CASE(T, D) return rel ? fwd<T, D, true>(a, s) : fwd<T, D, false>(a, s)
+  const bool narrow = a.q_rows == kNarrowRows;
+#define TX_CASE(T, D)                                                                   \
+  return narrow ? (rel ? fwd<T, D, true, true>(a, s) : fwd<T, D, false, true>(a, s))    \
+                : (rel ? fwd<T, D, true, false>(a, s) : fwd<T, D, false, false>(a, s))
   if (bf) {
     if (dh == 32) TX_CASE(bf16, 32);
     if (dh == 64) TX_CASE(bf16, 64);
