@@ -5,6 +5,15 @@
 
 namespace tx {
 
+// Row offsets base, base + len[0], base + len[0] + len[1], .. (n lengths, n + 1
+// offsets) as kernel arguments.
+struct PrefOffsets {
+  static constexpr int kLengths = 1536;
+  int32_t base, n;
+  uint16_t len[kLengths];
+};
+hipError_t launch_pref_offsets(int32_t* dst, const PrefOffsets& a, hipStream_t s);
+
 // Per row r of row0 .. row0 + n - 1 with logits z [k] (k = 1: the scalar logit
 // s, read as [0, s]): row_lse[r] = log sum exp z and picked[r - row0] = z[act] -
 // lse, 0 for rows whose action lies outside the vocabulary or whose logits are

@@ -20,6 +20,36 @@ constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float to_f(bf16 x) { return (float)x; }
 __device__ __forceinline__ float to_f(float x) { return x; }
 
+__global__ __launch_bounds__(256) void pref_offsets_kernel(int32_t* __restrict__ dst, const PrefOffsets a) {
+  // thread t sums lengths t * per .. , the block scans the threads' sums
+  constexpr int per = PrefOffsets::kLengths / 256;
+  __shared__ int32_t sums[4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  int32_t len[per], own = 0;
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const int k = tid * per + i;
+    len[i] = k < a.n ? a.len[k] : 0;
+    own += len[i];
+  }
+  int32_t up_to = own;  // inclusive over the wave
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t x = __shfl_up(up_to, d);
+    if (lane >= d) up_to += x;
+  }
+  if (lane == 63) sums[tid >> 6] = up_to;
+  __syncthreads();
+  int32_t at = a.base + up_to - own;
+  for (int w = 0; w < (tid >> 6); ++w) at += sums[w];
+  if (tid == 0) dst[0] = a.base;
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    at += len[i];
+    if (tid * per + i < a.n) dst[tid * per + i + 1] = at;
+  }
+}
+
 // (max, sum of exp(x - max)) of two disjoint sets; empty: (-inf, 0).
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   const float top = fmaxf(m, m2);
@@ -99,26 +129,34 @@ __global__ __launch_bounds__(256) void pref_rows_wide(const T* __restrict__ z, i
   const T* const p = z + row * ld;
   const int head = head_of(p, k), nv = (k - head) / N, tail = head + nv * N;
   float m = -INFINITY, s = 0.f;
-  auto take = [&](const Vec<T>& v) {
-    float x[N], top = m;
+  auto take = [&](const auto& vs) {
+    constexpr int V = sizeof(vs) / sizeof(vs[0]);
+    float x[V * N], top = m;
 #pragma unroll
-    for (int t = 0; t < N; ++t) x[t] = to_f(v.x[t]), top = fmaxf(top, x[t]);
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int t = 0; t < N; ++t) x[i * N + t] = to_f(vs[i].x[t]), top = fmaxf(top, x[i * N + t]);
     const float ref = top == -INFINITY ? 0.f : top;
     s *= __builtin_amdgcn_exp2f((m - ref) * kLog2e);
 #pragma unroll
-    for (int t = 0; t < N; ++t) s += __builtin_amdgcn_exp2f((x[t] - ref) * kLog2e);
+    for (int i = 0; i < V * N; ++i) s += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
     m = top;
   };
   for (int e = tid; e < head; e += 256) join(m, s, to_f(p[e]), 1.f);
   for (int e = tail + tid; e < k; e += 256) join(m, s, to_f(p[e]), 1.f);
+  // eight 16-byte loads of a thread in flight, rescaled once for all eight
   const T* const q = p + head;
   int v = tid;
-  for (; v + 768 < nv; v += 1024) {
-    const Vec<T> a0 = load_vec(q + (int64_t)v * N), a1 = load_vec(q + (int64_t)(v + 256) * N),
-                 a2 = load_vec(q + (int64_t)(v + 512) * N), a3 = load_vec(q + (int64_t)(v + 768) * N);
-    take(a0), take(a1), take(a2), take(a3);
+  for (; v + 7 * 256 < nv; v += 8 * 256) {
+    Vec<T> a[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = load_vec(q + (int64_t)(v + 256 * i) * N);
+    take(a);
   }
-  for (; v < nv; v += 256) take(load_vec(q + (int64_t)v * N));
+  for (; v < nv; v += 256) {
+    const Vec<T> a[1] = {load_vec(q + (int64_t)v * N)};
+    take(a);
+  }
   const float top = wave_max(m);
   const float ref = top == -INFINITY ? 0.f : top;
   s = wave_sum(s * __builtin_amdgcn_exp2f((m - ref) * kLog2e));
@@ -210,7 +248,8 @@ __global__ __launch_bounds__(256) void pref_grad_wide(const T* __restrict__ z, i
                                                      T* __restrict__ dz, int64_t ldd) {
   constexpr int N = Vec<T>::N;
   const int tid = threadIdx.x;
-  const int64_t i = blockIdx.x, row = row0 + i;
+  // last row first: what the forward read last may still be in the caches
+  const int64_t i = (int64_t)gridDim.x - 1 - blockIdx.x, row = row0 + i;
   const T* const p = z + row * ld;
   T* const o = dz + row * ldd;
   const int a = act[row];
@@ -273,6 +312,10 @@ hipError_t grad(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0,
 
 }  // namespace
 
+hipError_t launch_pref_offsets(int32_t* dst, const PrefOffsets& a, hipStream_t s) {
+  pref_offsets_kernel<<<1, 256, 0, s>>>(dst, a);
+  return hipGetLastError();
+}
 hipError_t launch_pref_rows(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
                             int64_t n, float* row_lse, float* picked, hipStream_t s) {
   return bf ? rows((const bf16*)logits, ld, k, act, row0, n, row_lse, picked, s)

@@ -314,7 +314,14 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   TX_CHECK(check_stream(st));
 
   char* const w = (char*)ws;
-  TX_HIP(put_all(w, p.meta, st));
+  const bool limits = !rel && p.tiles > 0, in_one = limits && p.meta.size() <= sizeof(MetaArg);
+  int32_t* const row_lim = (int32_t*)(w + p.at.row_lim);
+  TileLim* const tile_lim = (TileLim*)(w + p.at.tile_lim);
+  if (in_one)
+    TX_HIP(launch_train_put_limits(w, p.meta.data(), p.meta.size(), (int32_t)p.groups.size(), (int32_t)p.tiles, p.o_row,
+                                   p.o_prefix, row_lim, (int32_t)p.q_base, tile_lim, st));
+  else
+    TX_HIP(put_all(w, p.meta, st));
   a.groups = (const TrainGroup*)w;
   a.n_groups = (int32_t)p.groups.size();
   a.n_units = (int32_t)p.units_q;
@@ -325,18 +332,17 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   a.row_stat = (float*)(w + p.at.stat);
   a.rel = x.rel;
   a.R = R;
-  a.row_lim = (const int32_t*)(w + p.at.row_lim);
-  a.tile_lim = (const TileLim*)(w + p.at.tile_lim);
+  a.row_lim = row_lim;
+  a.tile_lim = tile_lim;
   a.q_base = (int32_t)p.q_base;
   a.scale = c.scale > 0.f ? c.scale : (float)(1.0 / std::sqrt((double)dh));
   a.scale_log2 = (float)(a.scale * 1.4426950408889634);
   a.partial = (float*)(w + p.at.partial);
   a.q_rows = p.q_rows, a.k_rows = p.k_rows;
   a.drel_part = (float*)(w + p.at.drel);
-  if (!rel)
+  if (limits && !in_one)
     TX_HIP(launch_train_limits(a.groups, a.n_groups, (int32_t)p.tiles, (const int32_t*)(w + p.o_row),
-                               (const int32_t*)(w + p.o_prefix), (int32_t*)(w + p.at.row_lim), a.q_base,
-                               (TileLim*)(w + p.at.tile_lim), st));
+                               (const int32_t*)(w + p.o_prefix), row_lim, a.q_base, tile_lim, st));
   // algorithmic work: 2 d_h flops per pair and product, each tensor once
   const double prod = 2.0 * dh * H * p.pairs, qb = (double)es * dh * H * p.rows_q, kb = (double)es * dh * G * p.rows_k;
   const double stat = 4.0 * H * p.rows_q;
@@ -368,7 +374,6 @@ int check_pref(const tx_preference_config* c, int32_t n, const int64_t* off) {
 }
 
 struct PrefPlan {
-  std::vector<char> meta;
   size_t at_row = 0, bytes = 0;
   int64_t row0 = 0, rows = 0;
 };
@@ -376,11 +381,28 @@ struct PrefPlan {
 void plan_pref(int32_t n, const int64_t* off, PrefPlan& p) {
   p.row0 = off[0];
   p.rows = off[2 * (int64_t)n] - off[0];
-  p.meta.resize((2 * (size_t)n + 1) * 4);
-  int32_t* o = (int32_t*)p.meta.data();
-  for (int64_t i = 0; i <= 2 * (int64_t)n; ++i) o[i] = (int32_t)(off[i] - off[0]);
-  p.at_row = align_up(p.meta.size());
+  p.at_row = align_up((2 * (size_t)n + 1) * 4);
   p.bytes = align_up(p.at_row + p.rows * 4 + 256);
+}
+
+// The answers' row offsets (from the first) on the device: lengths of 16 bits as
+// kernel arguments, summed up there, twice as many a launch as offsets would be;
+// offsets where an answer is longer.
+hipError_t put_answer_offsets(int32_t* dst, const int64_t* off, int64_t n, hipStream_t s) {
+  for (int64_t i = 0; i <= n;) {
+    PrefOffsets a;
+    a.base = (int32_t)(off[i] - off[0]);
+    int32_t m = 0;  // offsets i .. i + m: one more than lengths
+    while (m < PrefOffsets::kLengths && i + m < n && off[i + m + 1] - off[i + m] <= 0xffff) {
+      a.len[m] = (uint16_t)(off[i + m + 1] - off[i + m]);
+      ++m;
+    }
+    a.n = m;
+    const hipError_t e = launch_pref_offsets(dst + i, a, s);
+    if (e != hipSuccess) return e;
+    i += m + 1;
+  }
+  return hipSuccess;
 }
 
 int check_pref_tensors(const tx_preference_config* c, const PrefPlan& p, const void* logits, int64_t ld,
@@ -494,7 +516,7 @@ int tx_preference_forward(const tx_preference_config* cfg, int32_t n, const int6
     if ((uintptr_t)ref_logp & 3) return fail(TX_E_INVALID, "ref_logp is misaligned");
     TX_CHECK(check_ws(ws, ws_bytes, p.bytes));
     TX_CHECK(check_stream(st));
-    TX_HIP(put_all((char*)ws, p.meta, st));
+    TX_HIP(put_answer_offsets((int32_t*)ws, off, 2 * (int64_t)n, st));
     float* const picked = (float*)((char*)ws + p.at_row);
     const bool bf = cfg->dtype == TX_BF16;
     const double nk = (double)p.rows * cfg->n_actions;
@@ -527,7 +549,7 @@ int tx_preference_backward(const tx_preference_config* cfg, int32_t n, const int
       return fail(TX_E_INVALID, "d_logits row stride %lld", (long long)d_row_stride);
     TX_CHECK(check_ws(ws, ws_bytes, p.bytes));
     TX_CHECK(check_stream(st));
-    TX_HIP(put_all((char*)ws, p.meta, st));
+    TX_HIP(put_answer_offsets((int32_t*)ws, off, 2 * (int64_t)n, st));
     float* const coef = (float*)((char*)ws + p.at_row);
     const double nk = (double)p.rows * cfg->n_actions;
     TX_LAUNCH(K_TRAIN_PREF, 0, 4.0 * p.rows,

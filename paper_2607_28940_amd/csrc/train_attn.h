@@ -17,6 +17,8 @@
 #include "tx_internal.h"
 #include "wave_reduce.h"
 
+#include <mutex>
+
 namespace tx {
 
 // A group of a call, rows counted from the start of the tensors. Units are the
@@ -83,10 +85,15 @@ hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32
 hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
 // drel[h][b] from the units' sums; scratch: [chunks][H][R] floats, chunks = ceil(units / 32)
 hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s);
-// row_lim and tile_lim of the event form from the events' row offsets and prefixes
+// row_lim and tile_lim of the event form (n_tiles > 0) from the groups and the
+// events' row offsets and prefixes: from memory, or from metadata of at most
+// sizeof(MetaArg) bytes (groups first) that is written to dst by the way
 hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
                                const int32_t* ev_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
                                hipStream_t s);
+hipError_t launch_train_put_limits(void* dst, const void* meta, size_t bytes, int32_t n_groups, int32_t n_tiles,
+                                   size_t o_row, size_t o_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
+                                   hipStream_t s);
 
 // floats of one partial slot
 __host__ __device__ inline size_t train_fwd_slot(int rows, int dh) { return (size_t)rows * (dh + 2); }
@@ -626,10 +633,23 @@ __device__ __forceinline__ void stage_bias(lds_float* tab, const T* __restrict__
   for (int i = tid; i < bias_entries(R); i += 256) tab[i] = bias_value(rel, R, h, i - kBiasPad);
 }
 
-// Lets a kernel use more than 64 KB of LDS a block.
-inline hipError_t allow_lds(const void* kernel, size_t bytes) {
-  return bytes <= 65536 ? hipSuccess
-                        : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+// Lets a kernel use more than 64 KB of LDS a block: remembers the most that it
+// was allowed on each device, and never lowers it.
+struct LdsAllowed {
+  std::mutex mu;
+  size_t bytes[64] = {};
+};
+inline hipError_t allow_lds(const void* kernel, size_t bytes, LdsAllowed& so_far) {
+  if (bytes <= 65536) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(so_far.mu);
+  if (so_far.bytes[dev] >= bytes) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == hipSuccess) so_far.bytes[dev] = bytes;
+  return e;
 }
 
 #endif  // __HIPCC__

@@ -342,7 +342,8 @@ template <class T, int DH, bool REL, bool NARROW>
 hipError_t dkv_launch(const TrainArgs& a, int32_t n_units, hipStream_t s) {
   const size_t lds = dkv_lds_bytes<T, DH, NARROW>() + 4 * stat_floats<T, DH, NARROW>() +
                      (REL ? 4 * (size_t)bias_entries(a.R) : 0);
-  const hipError_t e = allow_lds((const void*)train_dkv_kernel<T, DH, REL, NARROW>, lds);
+  static LdsAllowed so_far;
+  const hipError_t e = allow_lds((const void*)train_dkv_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
   train_dkv_kernel<T, DH, REL, NARROW><<<dim3((unsigned)n_units * a.G), 256, lds, s>>>(a);
   return hipGetLastError();

@@ -334,7 +334,8 @@ template <class T, int DH, bool REL, bool NARROW>
 hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
   const size_t lds =
       dq_lds_bytes<T, DH, NARROW>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 5 : 1) : 0);
-  const hipError_t e = allow_lds((const void*)train_dq_kernel<T, DH, REL, NARROW>, lds);
+  static LdsAllowed so_far;
+  const hipError_t e = allow_lds((const void*)train_dq_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
   train_dq_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
   return hipGetLastError();

@@ -1,6 +1,7 @@
 // Forward of the training attention (train_attn.h): O and lse of 128 queries of
 // one (group, head) per block, in one pass over the visible keys with the
 // running maximum and sum of the softmax.
+#include "meta_put.h"
 #include "train_attn.h"
 
 #include <type_traits>
@@ -351,13 +352,11 @@ __global__ __launch_bounds__(256) void train_fwd_join_kernel(const TrainArgs a) 
 }
 
 // The event form's key limits: a wave per 64-row query tile finds each row's
-// event (the last whose first row is not past it: events may be empty) and keeps its prefix, with
-// the tile's smallest and largest.
-__global__ __launch_bounds__(64) void train_limits_kernel(const TrainGroup* __restrict__ groups, int n_groups,
-                                                         const int32_t* __restrict__ ev_row,
-                                                         const int32_t* __restrict__ ev_prefix,
-                                                         int32_t* __restrict__ row_lim, int q_base,
-                                                         TileLim* __restrict__ tile_lim) {
+// event (the last whose first row is not past it: events may be empty) and keeps
+// its prefix, with the tile's smallest and largest.
+__device__ __forceinline__ void key_limits(const TrainGroup* groups, int n_groups, const int32_t* ev_row,
+                                           const int32_t* ev_prefix, int32_t* __restrict__ row_lim, int q_base,
+                                           TileLim* __restrict__ tile_lim) {
   const int lane = threadIdx.x, tile = blockIdx.x;
   // the last group whose first tile is not past this one
   int lo = 0, n = n_groups;
@@ -392,10 +391,29 @@ __global__ __launch_bounds__(64) void train_limits_kernel(const TrainGroup* __re
   if (lane == 0) tile_lim[tile] = TileLim{mn, mx};
 }
 
+__global__ __launch_bounds__(64) void train_limits_kernel(const TrainGroup* __restrict__ groups, int n_groups,
+                                                         const int32_t* __restrict__ ev_row,
+                                                         const int32_t* __restrict__ ev_prefix, int32_t* row_lim,
+                                                         int q_base, TileLim* tile_lim) {
+  key_limits(groups, n_groups, ev_row, ev_prefix, row_lim, q_base, tile_lim);
+}
+
+// The same from metadata that comes as arguments, which the launch also writes
+// to where the next ones read it: one launch instead of two.
+__global__ __launch_bounds__(64) void train_put_limits_kernel(uint32_t* __restrict__ dst, int words, int n_groups,
+                                                             int o_row, int o_prefix, int32_t* row_lim, int q_base,
+                                                             TileLim* tile_lim, const MetaArg m) {
+  for (int i = blockIdx.x * 64 + threadIdx.x; i < words; i += gridDim.x * 64) dst[i] = m.w[i];
+  const char* const src = (const char*)m.w;
+  key_limits((const TrainGroup*)src, n_groups, (const int32_t*)(src + o_row), (const int32_t*)(src + o_prefix), row_lim,
+             q_base, tile_lim);
+}
+
 template <class T, int DH, bool REL, bool NARROW>
 hipError_t fwd(const TrainArgs& a, hipStream_t s) {
   const size_t lds = fwd_lds_bytes<T, DH, NARROW>() + (REL ? 4 * (size_t)bias_entries(a.R) : 0);
-  const hipError_t e = allow_lds((const void*)train_fwd_kernel<T, DH, REL, NARROW>, lds);
+  static LdsAllowed so_far;
+  const hipError_t e = allow_lds((const void*)train_fwd_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
   train_fwd_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
   return hipGetLastError();
@@ -434,8 +452,19 @@ hipError_t launch_train_fwd_join(bool bf, int dh, const TrainArgs& a, hipStream_
 hipError_t launch_train_limits(const TrainGroup* groups, int32_t n_groups, int32_t n_tiles, const int32_t* ev_row,
                                const int32_t* ev_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
                                hipStream_t s) {
-  if (n_tiles == 0) return hipSuccess;
   train_limits_kernel<<<n_tiles, 64, 0, s>>>(groups, n_groups, ev_row, ev_prefix, row_lim, q_base, tile_lim);
+  return hipGetLastError();
+}
+
+hipError_t launch_train_put_limits(void* dst, const void* meta, size_t bytes, int32_t n_groups, int32_t n_tiles,
+                                   size_t o_row, size_t o_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
+                                   hipStream_t s) {
+  MetaArg m;
+  memcpy(m.w, meta, bytes);
+  const int words = (int)((bytes + 3) / 4);
+  if (bytes % 4) memset((char*)m.w + bytes, 0, 4 - bytes % 4);
+  train_put_limits_kernel<<<n_tiles, 64, 0, s>>>((uint32_t*)dst, words, n_groups, (int)o_row, (int)o_prefix, row_lim,
+                                                 q_base, tile_lim, m);
   return hipGetLastError();
 }
 

@@ -97,21 +97,21 @@ _SIGS = {
     "score_candidates": (ctypes.c_int, [VP, ctypes.c_int32, I32P, VP, I64P, VP, I64P, VP, VP, ctypes.c_size_t, VP]),
     "score_candidates_static": (ctypes.c_int, [VP, ctypes.c_int32, I32P, VP, I64P, VP, I64P, VP, VP]),
     "score_events": (ctypes.c_int, [VP, ctypes.c_int32, I32P, I64P, VP, I64P, VP, I64P, VP, VP, ctypes.c_size_t, VP]),
-    "tx_rel_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, I64P]),
-    "tx_rel_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
+    "tx_rel_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, VP]),
+    "tx_rel_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, VP, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
                                            ctypes.c_int64, VP, ctypes.c_size_t, VP]),
-    "tx_rel_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
+    "tx_rel_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, VP, ROWSP, ROWSP, ROWSP, VP, ROWSP, VP,
                                             ctypes.c_int64, ROWSP, ROWSP, ROWSP, ROWSP, VP, VP, ctypes.c_size_t, VP]),
-    "tx_event_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, I64P, I64P, I64P, I64P]),
-    "tx_event_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, I64P, I64P, I64P, ROWSP, ROWSP, ROWSP,
+    "tx_event_attn_workspace_bytes": (ctypes.c_size_t, [ACFGP, ctypes.c_int32, ctypes.c_int32, VP, VP, VP, VP]),
+    "tx_event_attn_forward": (ctypes.c_int, [ACFGP, ctypes.c_int32, VP, VP, VP, VP, ROWSP, ROWSP, ROWSP,
                                              ROWSP, VP, ctypes.c_int64, VP, ctypes.c_size_t, VP]),
-    "tx_event_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, I64P, I64P, I64P, I64P, ROWSP, ROWSP, ROWSP,
+    "tx_event_attn_backward": (ctypes.c_int, [ACFGP, ctypes.c_int32, VP, VP, VP, VP, ROWSP, ROWSP, ROWSP,
                                               ROWSP, VP, ctypes.c_int64, ROWSP, ROWSP, ROWSP, ROWSP, VP,
                                               ctypes.c_size_t, VP]),
-    "tx_preference_workspace_bytes": (ctypes.c_size_t, [PCFGP, ctypes.c_int32, I64P]),
-    "tx_preference_forward": (ctypes.c_int, [PCFGP, ctypes.c_int32, I64P, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
+    "tx_preference_workspace_bytes": (ctypes.c_size_t, [PCFGP, ctypes.c_int32, VP]),
+    "tx_preference_forward": (ctypes.c_int, [PCFGP, ctypes.c_int32, VP, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
                                              ctypes.c_size_t, VP]),
-    "tx_preference_backward": (ctypes.c_int, [PCFGP, ctypes.c_int32, I64P, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
+    "tx_preference_backward": (ctypes.c_int, [PCFGP, ctypes.c_int32, VP, VP, ctypes.c_int64, VP, VP, VP, VP, VP, VP,
                                               ctypes.c_int64, VP, ctypes.c_size_t, VP]),
     "tx_profile_enable": (ctypes.c_int, [ctypes.c_int32]),
     "tx_profile_select": (ctypes.c_int, [ctypes.c_uint64]),
@@ -354,17 +354,18 @@ def _invalid(msg: str):
 class _On:
     """The tensors' device and the call's stream, current for the call."""
 
-    def __init__(self, tensors: dict, stream):
+    def __init__(self, names: str, tensors, stream):
         import torch
         dev = None
-        for name, t in tensors.items():
+        for i, t in enumerate(tensors):
             if t is None:
                 continue
-            if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
-                _invalid(f"{name} is not a GPU tensor")
-            if dev is not None and t.device != dev:
-                _invalid(f"{name} is on {t.device}, other tensors are on {dev}")
-            dev = t.device
+            if not (isinstance(t, torch.Tensor) and t.is_cuda):
+                _invalid(f"{names.split()[i]} is not a GPU tensor")
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                _invalid(f"{names.split()[i]} is on {t.device}, other tensors are on {dev}")
         if stream is not None and stream.device != dev:
             _invalid(f"the stream belongs to {stream.device}, the tensors are on {dev}")
         self.dev, self.ctx = dev, None
@@ -372,12 +373,13 @@ class _On:
             self.ctx = torch.cuda.stream(stream)
         elif dev.index != torch.cuda.current_device():
             self.ctx = torch.cuda.device(dev)
+        self.empty, self.uint8 = torch.empty, torch.uint8
+        self.current = torch.cuda.current_stream
 
     def __enter__(self):
-        import torch
         if self.ctx is not None:
             self.ctx.__enter__()
-        self.stream = VP(torch.cuda.current_stream().cuda_stream)
+        self.stream = self.current(self.dev).cuda_stream
         return self
 
     def __exit__(self, *exc):
@@ -385,9 +387,8 @@ class _On:
             self.ctx.__exit__(*exc)
 
     def workspace(self, nbytes: int):
-        import torch
         # (0: the size function refused the arguments, and the call will say why)
-        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
+        return self.empty(max(nbytes, 256), dtype=self.uint8, device=self.dev)
 
 
 def _heads(t, name: str, dtype, shape=None) -> Rows:
@@ -396,19 +397,20 @@ def _heads(t, name: str, dtype, shape=None) -> Rows:
         _invalid(f"{name} must be [rows, heads, d_head]")
     if t.dtype != dtype:
         _invalid(f"{name} is {t.dtype}, q is {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _invalid(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.shape[2] > 1 and t.stride(2) != 1 and t.numel():
+    n, h, d = t.shape
+    if shape is not None and (n, h, d) != tuple(shape):
+        _invalid(f"{name} is {(n, h, d)}, expected {tuple(shape)}")
+    row, head, one = t.stride()
+    if one != 1 and d > 1 and n * h:
         _invalid(f"{name}: features of a head must be contiguous")
     # (torch leaves the stride of a single row or head to chance)
-    head = t.stride(1) if t.shape[1] > 1 else t.shape[2]
-    return Rows(t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], head)
+    return Rows(t.data_ptr(), row if n > 1 else h * d, head if h > 1 else d)
 
 
-def _plain(t, name: str, dtype, shape):
+def _plain(t, name: str, dtype, shape) -> int:
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         _invalid(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
-    return VP(t.data_ptr() or None)
+    return t.data_ptr()
 
 
 def _dtype_of(t, name: str) -> int:
@@ -440,9 +442,15 @@ def _offsets(a, name: str, n: Optional[int] = None) -> np.ndarray:
     return a
 
 
-def _covers(rows: int, off: np.ndarray, name: str):
+def _at(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
+
+
+def _covers(rows: int, off: np.ndarray, name: str) -> bool:
+    """Whether the offsets take every row; refuses offsets past the last."""
     if off[-1] > rows:
         _invalid(f"{name} offsets reach row {int(off[-1])} of {rows}")
+    return bool(off[0] == 0 and off[-1] == rows)
 
 
 def _new_like(t, rows_used: bool):
@@ -457,8 +465,9 @@ def _new_lse(H: int, M: int, full: bool, dev):
         torch.full((H, M), -float("inf"), dtype=torch.float32, device=dev)
 
 
-def _whole(off: np.ndarray, rows: int) -> bool:
-    return off[0] == 0 and off[-1] == rows
+def _f32():
+    import torch
+    return torch.float32
 
 
 def rel_attention(q, k, v, rel, offsets, scale: Optional[float] = None, out=None, lse=None, stream=None):
@@ -468,21 +477,17 @@ def rel_attention(q, k, v, rel, offsets, scale: Optional[float] = None, out=None
     and lse fp32 [heads, rows]; rows outside the offsets keep what `out` and
     `lse` held (0 and -inf where this call makes them)."""
     off = _offsets(offsets, "sequence offsets")
-    with _On(dict(q=q, k=k, v=v, rel=rel, out=out, lse=lse), stream) as on:
+    with _On("q k v rel out lse", (q, k, v, rel, out, lse), stream) as on:
         cfg = _attn_config(q, k, rel, scale)
-        M, H = q.shape[0], q.shape[1]
-        kv = (M,) + tuple(k.shape[1:])
-        _covers(M, off, "sequence")
-        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype, kv), _heads(v, "v", q.dtype, kv)]
-        if out is None:
-            out = _new_like(q, _whole(off, M))
-        if lse is None:
-            lse = _new_lse(H, M, _whole(off, M), on.dev)
-        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
-        L, n, op = lib(), len(off) - 1, _p(off, I64P)
-        ws = on.workspace(L.tx_rel_attn_workspace_bytes(ctypes.byref(cfg), 0, n, op))
-        check(L.tx_rel_attn_forward(ctypes.byref(cfg), n, op, *map(ctypes.byref, a), _rel_ptr(rel), ctypes.byref(o), l,
-                                    M, VP(ws.data_ptr()), ws.numel(), on.stream))
+        M, H, dt = q.shape[0], q.shape[1], q.dtype
+        whole, kv = _covers(M, off, "sequence"), (M, k.shape[1], k.shape[2])
+        out = _new_like(q, whole) if out is None else out
+        lse = _new_lse(H, M, whole, on.dev) if lse is None else lse
+        L, n, op = lib(), len(off) - 1, _at(off)
+        ws = on.workspace(L.tx_rel_attn_workspace_bytes(cfg, 0, n, op))
+        check(L.tx_rel_attn_forward(cfg, n, op, _heads(q, "q", dt), _heads(k, "k", dt, kv), _heads(v, "v", dt, kv),
+                                    rel.data_ptr() if rel is not None else None, _heads(out, "out", dt, q.shape),
+                                    _plain(lse, "lse", _f32(), (H, M)), M, ws.data_ptr(), ws.numel(), on.stream))
     return out, lse
 
 
@@ -490,46 +495,32 @@ def rel_attention_backward(dout, q, k, v, rel, out, lse, offsets, scale: Optiona
                            dv=None, drel=None, stream=None):
     """Gradients of rel_attention for dout, given its inputs and outputs
     (tx_rel_attn_backward): dq, dk, dv and drel (None without a bias)."""
-    import torch
     off = _offsets(offsets, "sequence offsets")
-    with _On(dict(q=q, k=k, v=v, rel=rel, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, drel=drel), stream) as on:
+    with _On("q k v rel out lse dout dq dk dv drel", (q, k, v, rel, out, lse, dout, dq, dk, dv, drel), stream) as on:
         cfg = _attn_config(q, k, rel, scale)
-        M, H = q.shape[0], q.shape[1]
-        kv = (M,) + tuple(k.shape[1:])
-        _covers(M, off, "sequence")
-        whole = _whole(off, M)
+        M, H, dt = q.shape[0], q.shape[1], q.dtype
+        whole, kv = _covers(M, off, "sequence"), (M, k.shape[1], k.shape[2])
         dq = _new_like(q, whole) if dq is None else dq
         dk = _new_like(k, whole) if dk is None else dk
         dv = _new_like(v, whole) if dv is None else dv
-        if rel is not None and drel is None:
-            drel = torch.empty_like(rel)
-        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype, kv), _heads(v, "v", q.dtype, kv)]
-        g = [_heads(dout, "dout", q.dtype, q.shape), _heads(dq, "dq", q.dtype, q.shape),
-             _heads(dk, "dk", q.dtype, kv), _heads(dv, "dv", q.dtype, kv)]
-        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
+        rel_at = drel_at = None
         if rel is not None:
-            _plain(drel, "drel", q.dtype, rel.shape)
-        L, n, op = lib(), len(off) - 1, _p(off, I64P)
-        ws = on.workspace(L.tx_rel_attn_workspace_bytes(ctypes.byref(cfg), 1, n, op))
-        check(L.tx_rel_attn_backward(ctypes.byref(cfg), n, op, *map(ctypes.byref, a), _rel_ptr(rel), ctypes.byref(o), l,
-                                     M, *map(ctypes.byref, g), _rel_ptr(drel if rel is not None else None),
-                                     VP(ws.data_ptr()), ws.numel(), on.stream))
+            drel = _new_like(rel, True) if drel is None else drel
+            rel_at, drel_at = rel.data_ptr(), _plain(drel, "drel", dt, rel.shape)
+        L, n, op = lib(), len(off) - 1, _at(off)
+        ws = on.workspace(L.tx_rel_attn_workspace_bytes(cfg, 1, n, op))
+        check(L.tx_rel_attn_backward(cfg, n, op, _heads(q, "q", dt), _heads(k, "k", dt, kv), _heads(v, "v", dt, kv),
+                                     rel_at, _heads(out, "out", dt, q.shape), _plain(lse, "lse", _f32(), (H, M)), M,
+                                     _heads(dout, "dout", dt, q.shape), _heads(dq, "dq", dt, q.shape),
+                                     _heads(dk, "dk", dt, kv), _heads(dv, "dv", dt, kv), drel_at, ws.data_ptr(),
+                                     ws.numel(), on.stream))
     return dq, dk, dv, (drel if rel is not None else None)
-
-
-def _f32():
-    import torch
-    return torch.float32
-
-
-def _rel_ptr(rel):
-    return VP(rel.data_ptr() or None) if rel is not None else VP()
 
 
 def _event_args(key_offsets, event_offsets, query_offsets, prefix_len):
     ko = _offsets(key_offsets, "key offsets")
     eo = _offsets(event_offsets, "event offsets", len(ko))
-    if eo[0] != 0 or np.any(np.diff(eo) < 0):
+    if eo[0] != 0 or (eo[1:] < eo[:-1]).any():
         _invalid("event offsets must start at 0 and not decrease")
     qo = _offsets(query_offsets, "query offsets", int(eo[-1]) + 1)
     pre = _i64(prefix_len)
@@ -545,20 +536,18 @@ def event_attention(q, k, v, key_offsets, event_offsets, query_offsets, prefix_l
     [query rows, heads, d_head], k and v [key rows, kv heads, d_head]. Returns
     out like q and lse fp32 [heads, query rows]."""
     where = _event_args(key_offsets, event_offsets, query_offsets, prefix_len)
-    with _On(dict(q=q, k=k, v=v, out=out, lse=lse), stream) as on:
+    with _On("q k v out lse", (q, k, v, out, lse), stream) as on:
         cfg = _attn_config(q, k, None, scale)
-        M, H = q.shape[0], q.shape[1]
-        _covers(M, where[2], "query")
+        M, H, dt = q.shape[0], q.shape[1], q.dtype
+        whole = _covers(M, where[2], "query")
         _covers(k.shape[0], where[0], "key")
-        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype), _heads(v, "v", q.dtype, k.shape)]
-        full = _whole(where[2], M)
-        out = _new_like(q, full) if out is None else out
-        lse = _new_lse(H, M, full, on.dev) if lse is None else lse
-        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
-        L, n, wp = lib(), len(where[0]) - 1, [_p(x, I64P) for x in where]
-        ws = on.workspace(L.tx_event_attn_workspace_bytes(ctypes.byref(cfg), 0, n, *wp))
-        check(L.tx_event_attn_forward(ctypes.byref(cfg), n, *wp, *map(ctypes.byref, a), ctypes.byref(o), l, M,
-                                      VP(ws.data_ptr()), ws.numel(), on.stream))
+        out = _new_like(q, whole) if out is None else out
+        lse = _new_lse(H, M, whole, on.dev) if lse is None else lse
+        L, n, wp = lib(), len(where[0]) - 1, [_at(x) for x in where]
+        ws = on.workspace(L.tx_event_attn_workspace_bytes(cfg, 0, n, *wp))
+        check(L.tx_event_attn_forward(cfg, n, *wp, _heads(q, "q", dt), _heads(k, "k", dt), _heads(v, "v", dt, k.shape),
+                                      _heads(out, "out", dt, q.shape), _plain(lse, "lse", _f32(), (H, M)), M,
+                                      ws.data_ptr(), ws.numel(), on.stream))
     return out, lse
 
 
@@ -567,22 +556,20 @@ def event_attention_backward(dout, q, k, v, out, lse, key_offsets, event_offsets
     """Gradients of event_attention for dout, given its inputs and outputs
     (tx_event_attn_backward): dq, dk, dv."""
     where = _event_args(key_offsets, event_offsets, query_offsets, prefix_len)
-    with _On(dict(q=q, k=k, v=v, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv), stream) as on:
+    with _On("q k v out lse dout dq dk dv", (q, k, v, out, lse, dout, dq, dk, dv), stream) as on:
         cfg = _attn_config(q, k, None, scale)
-        M, H = q.shape[0], q.shape[1]
-        _covers(M, where[2], "query")
-        _covers(k.shape[0], where[0], "key")
-        dq = _new_like(q, _whole(where[2], M)) if dq is None else dq
-        dk = _new_like(k, _whole(where[0], k.shape[0])) if dk is None else dk
-        dv = _new_like(v, _whole(where[0], k.shape[0])) if dv is None else dv
-        a = [_heads(q, "q", q.dtype), _heads(k, "k", q.dtype), _heads(v, "v", q.dtype, k.shape)]
-        g = [_heads(dout, "dout", q.dtype, q.shape), _heads(dq, "dq", q.dtype, q.shape),
-             _heads(dk, "dk", q.dtype, k.shape), _heads(dv, "dv", q.dtype, k.shape)]
-        o, l = _heads(out, "out", q.dtype, q.shape), _plain(lse, "lse", _f32(), (H, M))
-        L, n, wp = lib(), len(where[0]) - 1, [_p(x, I64P) for x in where]
-        ws = on.workspace(L.tx_event_attn_workspace_bytes(ctypes.byref(cfg), 1, n, *wp))
-        check(L.tx_event_attn_backward(ctypes.byref(cfg), n, *wp, *map(ctypes.byref, a), ctypes.byref(o), l, M,
-                                       *map(ctypes.byref, g), VP(ws.data_ptr()), ws.numel(), on.stream))
+        M, H, dt = q.shape[0], q.shape[1], q.dtype
+        whole, whole_k = _covers(M, where[2], "query"), _covers(k.shape[0], where[0], "key")
+        dq = _new_like(q, whole) if dq is None else dq
+        dk = _new_like(k, whole_k) if dk is None else dk
+        dv = _new_like(v, whole_k) if dv is None else dv
+        L, n, wp = lib(), len(where[0]) - 1, [_at(x) for x in where]
+        ws = on.workspace(L.tx_event_attn_workspace_bytes(cfg, 1, n, *wp))
+        check(L.tx_event_attn_backward(cfg, n, *wp, _heads(q, "q", dt), _heads(k, "k", dt), _heads(v, "v", dt, k.shape),
+                                       _heads(out, "out", dt, q.shape), _plain(lse, "lse", _f32(), (H, M)), M,
+                                       _heads(dout, "dout", dt, q.shape), _heads(dq, "dq", dt, q.shape),
+                                       _heads(dk, "dk", dt, k.shape), _heads(dv, "dv", dt, k.shape), ws.data_ptr(),
+                                       ws.numel(), on.stream))
     return dq, dk, dv
 
 
@@ -597,13 +584,13 @@ def _pref_args(logits, actions, offsets, beta, smoothing):
         _invalid("actions must be a contiguous int32 tensor with an entry per row")
     if logits.dim() == 2 and logits.shape[1] < 2:
         _invalid("logits need two actions or more (or [rows] for the scalar head)")
-    _covers(logits.shape[0], off, "answer")
+    whole = _covers(logits.shape[0], off, "answer")
     k = 1 if logits.dim() == 1 else logits.shape[1]
-    return off, PreferenceConfig(_dtype_of(logits, "logits"), k, float(beta), float(smoothing))
+    return off, PreferenceConfig(_dtype_of(logits, "logits"), k, float(beta), float(smoothing)), whole
 
 
 def _row_stride(t) -> int:
-    return max(t.stride(0), 1 if t.dim() == 1 else t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    return t.stride(0) if t.shape[0] > 1 else 1 if t.dim() == 1 else t.shape[1]
 
 
 def preference_loss(logits, actions, offsets, ref_logp=None, beta: float = 0.1, smoothing: float = 0.0, stream=None):
@@ -612,17 +599,17 @@ def preference_loss(logits, actions, offsets, ref_logp=None, beta: float = 0.1, 
     (2p preferred, 2p + 1 not), ref_logp fp32 [answers] or None. Returns loss
     fp32 [pairs], logp fp32 [answers] and row_lse fp32 [rows] (for the backward)."""
     import torch
-    with _On(dict(logits=logits, actions=actions, ref_logp=ref_logp), stream) as on:
-        off, cfg = _pref_args(logits, actions, offsets, beta, smoothing)
+    f32 = torch.float32
+    with _On("logits actions ref_logp", (logits, actions, ref_logp), stream) as on:
+        off, cfg, _ = _pref_args(logits, actions, offsets, beta, smoothing)
         P = len(off) // 2
-        ref = _plain(ref_logp, "ref_logp", torch.float32, (2 * P,)) if ref_logp is not None else VP()
-        loss, logp = (torch.empty(n, dtype=torch.float32, device=on.dev) for n in (P, 2 * P))
-        row_lse = torch.empty(logits.shape[0], dtype=torch.float32, device=on.dev)
-        L, op = lib(), _p(off, I64P)
-        ws = on.workspace(L.tx_preference_workspace_bytes(ctypes.byref(cfg), P, op))
-        check(L.tx_preference_forward(ctypes.byref(cfg), P, op, VP(logits.data_ptr()), _row_stride(logits),
-                                      VP(actions.data_ptr()), ref, VP(loss.data_ptr()), VP(logp.data_ptr()),
-                                      VP(row_lse.data_ptr()), VP(ws.data_ptr()), ws.numel(), on.stream))
+        ref = _plain(ref_logp, "ref_logp", f32, (2 * P,)) if ref_logp is not None else None
+        loss, logp, row_lse = (torch.empty(n, dtype=f32, device=on.dev) for n in (P, 2 * P, logits.shape[0]))
+        L, op = lib(), _at(off)
+        ws = on.workspace(L.tx_preference_workspace_bytes(cfg, P, op))
+        check(L.tx_preference_forward(cfg, P, op, logits.data_ptr(), _row_stride(logits), actions.data_ptr(), ref,
+                                      loss.data_ptr(), logp.data_ptr(), row_lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                      on.stream))
     return loss, logp, row_lse
 
 
@@ -630,24 +617,22 @@ def preference_loss_backward(dloss, logits, actions, offsets, ref_logp, logp, ro
                              smoothing: float = 0.0, dlogits=None, stream=None):
     """d_logits of preference_loss for dloss fp32 [pairs] (tx_preference_backward);
     rows outside the offsets keep what `dlogits` held (0 where this call makes it)."""
-    import torch
-    with _On(dict(logits=logits, actions=actions, ref_logp=ref_logp, logp=logp, row_lse=row_lse, dloss=dloss,
-                  dlogits=dlogits), stream) as on:
-        off, cfg = _pref_args(logits, actions, offsets, beta, smoothing)
-        P, M = len(off) // 2, logits.shape[0]
-        ref = _plain(ref_logp, "ref_logp", torch.float32, (2 * P,)) if ref_logp is not None else VP()
-        f = [_plain(logp, "logp", torch.float32, (2 * P,)), _plain(row_lse, "row_lse", torch.float32, (M,)),
-             _plain(dloss, "dloss", torch.float32, (P,))]
+    with _On("logits actions ref_logp logp row_lse dloss dlogits",
+             (logits, actions, ref_logp, logp, row_lse, dloss, dlogits), stream) as on:
+        off, cfg, whole = _pref_args(logits, actions, offsets, beta, smoothing)
+        P, M, f32 = len(off) // 2, logits.shape[0], _f32()
+        ref = _plain(ref_logp, "ref_logp", f32, (2 * P,)) if ref_logp is not None else None
         if dlogits is None:
-            dlogits = _new_like(logits, _whole(off, M))
+            dlogits = _new_like(logits, whole)
         if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or \
                 (dlogits.dim() == 2 and dlogits.stride(1) != 1):
             _invalid("dlogits must be like logits, actions contiguous")
-        L, op = lib(), _p(off, I64P)
-        ws = on.workspace(L.tx_preference_workspace_bytes(ctypes.byref(cfg), P, op))
-        check(L.tx_preference_backward(ctypes.byref(cfg), P, op, VP(logits.data_ptr()), _row_stride(logits),
-                                       VP(actions.data_ptr()), ref, *f, VP(dlogits.data_ptr()), _row_stride(dlogits),
-                                       VP(ws.data_ptr()), ws.numel(), on.stream))
+        L, op = lib(), _at(off)
+        ws = on.workspace(L.tx_preference_workspace_bytes(cfg, P, op))
+        check(L.tx_preference_backward(cfg, P, op, logits.data_ptr(), _row_stride(logits), actions.data_ptr(), ref,
+                                       _plain(logp, "logp", f32, (2 * P,)), _plain(row_lse, "row_lse", f32, (M,)),
+                                       _plain(dloss, "dloss", f32, (P,)), dlogits.data_ptr(), _row_stride(dlogits),
+                                       ws.data_ptr(), ws.numel(), on.stream))
     return dlogits
 
 
