@@ -19,9 +19,9 @@ hipError_t launch_pref_offsets(int32_t* dst, const PrefOffsets& a, hipStream_t s
 // lse, 0 for rows whose action lies outside the vocabulary or whose logits are
 // all minus infinity.
 hipError_t launch_pref_rows(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
-                            int64_t n, float* row_lse, float* picked, hipStream_t s);
+                            int64_t n, float* row_lse, double* picked, hipStream_t s);
 // Sums per answer (offs: 2 * n_pairs + 1 row offsets from row0) and the pairs' losses.
-hipError_t launch_pref_pairs(const float* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
+hipError_t launch_pref_pairs(const double* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
                              float eps, float* logp, float* loss, hipStream_t s);
 // coef[row - row0]: what a row's one-hot minus softmax is multiplied by.
 hipError_t launch_pref_coef(const int32_t* offs, int32_t n_pairs, const float* ref, const float* logp,

@@ -75,17 +75,21 @@ __device__ __forceinline__ int head_of(const T* row, int k) {
   return min(k, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));
 }
 
-__device__ __forceinline__ void finish_row(float m, float s, float z_act, bool counts, float* lse, float* picked) {
-  const float l = m == -INFINITY ? -INFINITY : m + logf(s);
-  *lse = l;
-  *picked = counts && l != -INFINITY ? z_act - l : 0.f;
+// An answer may have a thousand rows of a few nats each, of whose sum the margin
+// keeps a small difference: log p of a row is taken and summed in 64 bits, so that
+// only the roundings inside s (2^-24 of a row's terms) reach the loss.
+__device__ __forceinline__ void finish_row(float m, float s, float z_act, bool counts, float* lse, double* picked) {
+  const bool some = m != -INFINITY;
+  const double l = some ? (double)m + log((double)s) : 0.0;
+  *lse = some ? (float)l : -INFINITY;
+  *picked = counts && some ? (double)z_act - l : 0.0;
 }
 
 // k <= 64: W lanes (a power of two >= k) hold a row, one element each.
 template <class T>
 __global__ __launch_bounds__(256) void pref_rows_narrow(const T* __restrict__ z, int64_t ld, int k, int W,
                                                        const int32_t* __restrict__ act, int64_t row0, int64_t n,
-                                                       float* __restrict__ row_lse, float* __restrict__ picked) {
+                                                       float* __restrict__ row_lse, double* __restrict__ picked) {
   const int j = threadIdx.x & (W - 1);
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / W;
   const bool ok = i < n;
@@ -104,7 +108,7 @@ __global__ __launch_bounds__(256) void pref_rows_narrow(const T* __restrict__ z,
 template <class T>
 __global__ __launch_bounds__(256) void pref_rows_scalar(const T* __restrict__ z, int64_t ld,
                                                        const int32_t* __restrict__ act, int64_t row0, int64_t n,
-                                                       float* __restrict__ row_lse, float* __restrict__ picked) {
+                                                       float* __restrict__ row_lse, double* __restrict__ picked) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   const int a = act[row0 + i];
@@ -113,7 +117,7 @@ __global__ __launch_bounds__(256) void pref_rows_scalar(const T* __restrict__ z,
   // so that a sure answer keeps its digits
   const float tail = log1pf(expf(-fabsf(s)));
   row_lse[row0 + i] = fmaxf(s, 0.f) + tail;
-  picked[i] = a == 1 ? -(fmaxf(-s, 0.f) + tail) : a == 0 ? -(fmaxf(s, 0.f) + tail) : 0.f;
+  picked[i] = a == 1 ? -((double)fmaxf(-s, 0.f) + tail) : a == 0 ? -((double)fmaxf(s, 0.f) + tail) : 0.0;
 }
 
 // Wider rows: a block of 256 per row, 16 bytes a lane between the row's ragged
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(256) void pref_rows_scalar(const T* __restrict__ z,
 template <class T>
 __global__ __launch_bounds__(256) void pref_rows_wide(const T* __restrict__ z, int64_t ld, int k,
                                                      const int32_t* __restrict__ act, int64_t row0,
-                                                     float* __restrict__ row_lse, float* __restrict__ picked) {
+                                                     float* __restrict__ row_lse, double* __restrict__ picked) {
   __shared__ float sm[4], ss[4];
   constexpr int N = Vec<T>::N;
   const int tid = threadIdx.x;
@@ -176,23 +180,22 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
   return x;
 }
 
-__device__ __forceinline__ double margin_of(const float* logp2, const float* ref, int pair, float beta) {
+template <class L>
+__device__ __forceinline__ double margin_of(const L* logp2, const float* ref, int pair, float beta) {
   const double rw = ref ? (double)ref[2 * pair] : 0.0, rl = ref ? (double)ref[2 * pair + 1] : 0.0;
   return (double)beta * (((double)logp2[0] - rw) - ((double)logp2[1] - rl));
 }
 
-// A block of two waves per pair, a wave per answer. An answer may have a
-// thousand rows of a few nats each, of which the margin keeps a difference: the
-// sum is held in 64 bits.
-__global__ __launch_bounds__(128) void pref_pairs_kernel(const float* __restrict__ picked,
+// A block of two waves per pair, a wave per answer.
+__global__ __launch_bounds__(128) void pref_pairs_kernel(const double* __restrict__ picked,
                                                         const int32_t* __restrict__ offs, const float* ref, float beta,
                                                         float eps, float* __restrict__ logp, float* __restrict__ loss) {
-  __shared__ float both[2];
+  __shared__ double both[2];
   const int pair = blockIdx.x, w = threadIdx.x >> 6, lane = threadIdx.x & 63, ans = 2 * pair + w;
   double x = 0.0;
-  for (int r = offs[ans] + lane; r < offs[ans + 1]; r += 64) x += (double)picked[r];
+  for (int r = offs[ans] + lane; r < offs[ans + 1]; r += 64) x += picked[r];
   x = wave_sum_f64(x);
-  if (lane == 0) logp[ans] = both[w] = (float)x;
+  if (lane == 0) both[w] = x, logp[ans] = (float)x;
   __syncthreads();
   if (threadIdx.x == 0) {
     const double m = margin_of(both, ref, pair, beta);
@@ -283,7 +286,7 @@ int lanes_for(int k) {
 }
 
 template <class T>
-hipError_t rows(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0, int64_t n, float* lse, float* picked,
+hipError_t rows(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0, int64_t n, float* lse, double* picked,
                 hipStream_t s) {
   if (k == 1) {
     pref_rows_scalar<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(z, ld, act, row0, n, lse, picked);
@@ -317,11 +320,11 @@ hipError_t launch_pref_offsets(int32_t* dst, const PrefOffsets& a, hipStream_t s
   return hipGetLastError();
 }
 hipError_t launch_pref_rows(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
-                            int64_t n, float* row_lse, float* picked, hipStream_t s) {
+                            int64_t n, float* row_lse, double* picked, hipStream_t s) {
   return bf ? rows((const bf16*)logits, ld, k, act, row0, n, row_lse, picked, s)
             : rows((const float*)logits, ld, k, act, row0, n, row_lse, picked, s);
 }
-hipError_t launch_pref_pairs(const float* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
+hipError_t launch_pref_pairs(const double* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
                              float eps, float* logp, float* loss, hipStream_t s) {
   pref_pairs_kernel<<<n_pairs, 128, 0, s>>>(picked, offs, ref, beta, eps, logp, loss);
   return hipGetLastError();

@@ -178,3 +178,22 @@ def test_graph_and_stream():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, res))
+
+
+def test_differences_of_long_answers():
+    """Two answers of thousands of nats whose margin is a few: the sums and the
+    margin keep 64 bits, so only the errors of single rows remain."""
+    k, n = 3001, 700
+    gen = torch.Generator().manual_seed(9)
+    z = torch.randn(2 * n, k, generator=gen)
+    z[n:] = z[:n] + 0.003 * torch.randn(n, k, generator=gen)
+    act = torch.randint(0, k, (n,), generator=gen, dtype=torch.int32).repeat(2)
+    off = _off([n, n])
+    loss, _, _ = T.preference_loss(z.cuda(), act.cuda(), off, None, beta=1.0)
+    p = torch.log_softmax(z.double(), 1).gather(1, act.long()[:, None])[:, 0]
+    m = p[:n].sum() - p[n:].sum()
+    want = -torch.nn.functional.logsigmoid(m)
+    assert p[:n].sum().abs() > 4000 and m.abs() < 4
+    # a row's sum of exponentials: 12 terms a thread and their joins, 32 u32 of it at most; rows err
+    # independently, so the margin by sqrt(2 n) rows' errors
+    assert abs(float(loss[0].cpu().double() - want)) < 32 * U32 * np.sqrt(2 * n) + 8 * U32 * (1 + float(want))
