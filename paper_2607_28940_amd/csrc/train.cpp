@@ -164,6 +164,10 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   for (const TrainGroup& g : p.groups) wide_q += blocks_of(g.nq) * H, wide_k += blocks_of(g.nk) * G;
   p.q_rows = wide_q >= kWideGrid ? kWideRows : kNarrowRows;
   p.k_rows = wide_k >= kWideGrid ? kWideRows : kNarrowRows;
+  // a narrow block's tiles (128 KB at d_head 128) leave room for the bias sums of
+  // some 1300 buckets
+  if (backward && rel && train_dq_lds(c.dtype == TX_BF16, dh, c.rel_pos_buckets, p.q_rows) > kTrainMaxLds)
+    p.q_rows = kWideRows;
   int64_t steps_q = 0, steps_k = 0;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     const TrainGroup& g = p.groups[i];
@@ -382,7 +386,7 @@ void plan_pref(int32_t n, const int64_t* off, PrefPlan& p) {
   p.row0 = off[0];
   p.rows = off[2 * (int64_t)n] - off[0];
   p.at_row = align_up((2 * (size_t)n + 1) * 4);
-  p.bytes = align_up(p.at_row + p.rows * 4 + 256);
+  p.bytes = align_up(p.at_row + p.rows * 8 + 256);  // forward: doubles, backward: floats
 }
 
 // The answers' row offsets (from the first) on the device: lengths of 16 bits as
@@ -517,13 +521,13 @@ int tx_preference_forward(const tx_preference_config* cfg, int32_t n, const int6
     TX_CHECK(check_ws(ws, ws_bytes, p.bytes));
     TX_CHECK(check_stream(st));
     TX_HIP(put_answer_offsets((int32_t*)ws, off, 2 * (int64_t)n, st));
-    float* const picked = (float*)((char*)ws + p.at_row);
+    double* const picked = (double*)((char*)ws + p.at_row);
     const bool bf = cfg->dtype == TX_BF16;
     const double nk = (double)p.rows * cfg->n_actions;
     if (p.rows)
-      TX_LAUNCH(K_TRAIN_PREF, 3 * nk, nk * (bf ? 2 : 4) + 12.0 * p.rows,
+      TX_LAUNCH(K_TRAIN_PREF, 3 * nk, nk * (bf ? 2 : 4) + 16.0 * p.rows,
                 launch_pref_rows(bf, logits, row_stride, cfg->n_actions, actions, p.row0, p.rows, row_lse, picked, st));
-    TX_LAUNCH(K_TRAIN_PREF, 0, 4.0 * p.rows,
+    TX_LAUNCH(K_TRAIN_PREF, 0, 8.0 * p.rows,
               launch_pref_pairs(picked, (const int32_t*)ws, n, ref_logp, cfg->beta, cfg->smoothing, logp, loss, st));
     return TX_OK;
   });

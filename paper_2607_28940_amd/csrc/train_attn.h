@@ -100,6 +100,11 @@ __host__ __device__ inline size_t train_fwd_slot(int rows, int dh) { return (siz
 __host__ __device__ inline size_t train_dq_slot(int rows, int dh) { return (size_t)rows * dh; }
 __host__ __device__ inline size_t train_dkv_slot(int rows, int dh) { return (size_t)2 * rows * dh; }
 
+// LDS of a block of the dq kernel: its tiles and the bias tables of R buckets;
+// what a CU has for one block, less the compiler's own.
+size_t train_dq_lds(bool bf, int dh, int R, int rows);
+constexpr size_t kTrainMaxLds = 159 * 1024;
+
 #ifdef __HIPCC__
 
 constexpr float kTrainLog2e = 1.4426950408889634f, kTrainLn2 = 0.6931471805599453f;

@@ -330,10 +330,12 @@ __global__ __launch_bounds__(256) void drel_head_kernel(const float* __restrict_
   if (tid == 0) drel[(size_t)h * R + R - 1] = (T)(0.f - (wsum[0] + wsum[1] + wsum[2] + wsum[3]));
 }
 
+// The biases and, where there are sums to take, a table of them per wave.
+size_t table_bytes(int R) { return 4 * (size_t)bias_entries(R) * (R > 1 ? 5 : 1); }
+
 template <class T, int DH, bool REL, bool NARROW>
 hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
-  const size_t lds =
-      dq_lds_bytes<T, DH, NARROW>() + (REL ? 4 * (size_t)bias_entries(a.R) * (a.R > 1 ? 5 : 1) : 0);
+  const size_t lds = dq_lds_bytes<T, DH, NARROW>() + (REL ? table_bytes(a.R) : 0);
   static LdsAllowed so_far;
   const hipError_t e = allow_lds((const void*)train_dq_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
@@ -347,6 +349,20 @@ hipError_t dq_join(const TrainArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+size_t train_dq_lds(bool bf, int dh, int R, int rows) {
+  const bool narrow = rows == kNarrowRows;
+#define TX_CASE(T, D) return table_bytes(R) + (narrow ? dq_lds_bytes<T, D, true>() : dq_lds_bytes<T, D, false>())
+  if (bf) {
+    if (dh == 32) TX_CASE(bf16, 32);
+    if (dh == 64) TX_CASE(bf16, 64);
+    TX_CASE(bf16, 128);
+  }
+  if (dh == 32) TX_CASE(float, 32);
+  if (dh == 64) TX_CASE(float, 64);
+  TX_CASE(float, 128);
+#undef TX_CASE
+}
 
 hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
   const bool narrow = a.q_rows == kNarrowRows;

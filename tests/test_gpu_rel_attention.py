@@ -215,3 +215,14 @@ def test_same_bits_on_every_run_and_in_graphs():
         torch.cuda.synchronize()
         for g, res in graphs:
             assert all(torch.equal(first[n], res[n]) for n in first), turn
+
+
+@pytest.mark.parametrize("R", [1300, 1500, 2048])
+@pytest.mark.parametrize("dtype,dh", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 128)])
+def test_many_buckets(dtype, dh, R):
+    """The bias tables beside the tiles of a block that divides 32 rows over its waves."""
+    dt = DT[dtype]
+    off = _off([70, 400, 2100])
+    q, k, v, do, rel = _inputs(dt, int(off[-1]), 2, 1, dh, R, seed=R + dh)
+    worst = F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
+    log(f"rel {dtype} d_h {dh} R {R}: {worst}")
