@@ -446,9 +446,18 @@ __device__ __forceinline__ void load_row_frags(const char* row, bool exists, int
   }
 }
 
-// A wave's own copies have landed.
+// For a wave on its own: its copies have landed, and its reads of the tile before
+// are done, so that the next copies may go there (LDS reads and copies into LDS
+// are not ordered by themselves).
 __device__ __forceinline__ void tile_ready() {
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+// Its reads alone.
+__device__ __forceinline__ void tile_read() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   asm volatile("" ::: "memory");
 }
 

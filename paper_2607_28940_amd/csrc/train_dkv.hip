@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
         }
         if (k_wave < g.nk) tile(masked_c, now, b);
         if (!more) break;
-        if (BUFS == 1) fetch(h, t, 0);
+        if (BUFS == 1) tile_read(), fetch(h, t, 0);
         park_stat(st, t, BUFS == 2 ? b ^ 1 : 0);
         now = t;
       }

@@ -239,7 +239,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
       for (; t < end; t += STEP) {
         if (BUFS == 2 && t + STEP < t_end) fetch(t + STEP, b ^ 1);
         if (decltype(masked_c)::value ? t * KT < lim_hi : rows_here) tile(masked_c, t, b);
-        if (BUFS == 1 && t + STEP < t_end) fetch(t + STEP, 0);
+        if (BUFS == 1 && t + STEP < t_end) tile_read(), fetch(t + STEP, 0);
         ready();
         if (BUFS == 2) b ^= 1;
       }
@@ -300,15 +300,15 @@ __global__ __launch_bounds__(256) void train_dq_join_kernel(const TrainArgs a) {
 constexpr int kDrelChunk = 32;
 __global__ __launch_bounds__(256) void drel_chunk_kernel(const float* __restrict__ part, int n_units, int HR,
                                                          float* __restrict__ out) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
+  const int i = blockIdx.y * 256 + threadIdx.x;
   if (i >= HR) return;
-  const int u0 = blockIdx.y * kDrelChunk, n = min(kDrelChunk, n_units - u0);
+  const int u0 = blockIdx.x * kDrelChunk, n = min(kDrelChunk, n_units - u0);
   float v[kDrelChunk], x = 0.f;
 #pragma unroll
   for (int u = 0; u < kDrelChunk; ++u) v[u] = u < n ? part[(size_t)(u0 + u) * HR + i] : 0.f;
 #pragma unroll
   for (int u = 0; u < kDrelChunk; ++u) x += v[u];
-  out[(size_t)blockIdx.y * HR + i] = x;
+  out[(size_t)blockIdx.x * HR + i] = x;
 }
 // ... and of all chunks, the last bucket as minus the others: a block per head.
 template <class T>
@@ -392,7 +392,7 @@ hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* 
   int n = a.R > 1 ? a.n_units : 0;
   if (n > kDrelChunk) {
     const int chunks = (n + kDrelChunk - 1) / kDrelChunk;
-    drel_chunk_kernel<<<dim3((HR + 255) / 256, chunks), 256, 0, s>>>(part, n, HR, scratch);
+    drel_chunk_kernel<<<dim3(chunks, (HR + 255) / 256), 256, 0, s>>>(part, n, HR, scratch);
     part = scratch, n = chunks;
   }
   if (bf) drel_head_kernel<bf16><<<a.H, 256, 0, s>>>(part, n, a.H, a.R, (bf16*)drel);

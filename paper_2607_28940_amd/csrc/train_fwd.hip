@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
       for (; t < end; t += STEP) {
         if (BUFS == 2 && t + STEP < t_end) fetch(t + STEP, b ^ 1);
         if (decltype(masked_c)::value ? t * KT < lim_hi : rows_here) tile(masked_c, t, b);
-        if (BUFS == 1 && t + STEP < t_end) fetch(t + STEP, 0);
+        if (BUFS == 1 && t + STEP < t_end) tile_read(), fetch(t + STEP, 0);
         ready();
         if (BUFS == 2) b ^= 1;
       }
