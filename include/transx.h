@@ -395,7 +395,9 @@ int tx_event_attn_backward(const tx_attn_config* cfg, int32_t n_users, const int
  * the preferred one of pair p, answer 2p + 1 the other:
  *   logp[a] = sum over rows of log softmax(logits[row])[actions[row]]
  *   m = beta ((logp[2p] - ref_logp[2p]) - (logp[2p+1] - ref_logp[2p+1]))
- *   loss[p] = -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) */
+ *   loss[p] = -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m)
+ * (a smoothing of 0 or 1 leaves out the term it takes nothing of). n_pairs at
+ * most 2^24. Log probabilities and margins are taken in 64 bits. */
 typedef struct {
   int32_t dtype;     /* tx_dtype of logits and d_logits */
   int32_t n_actions; /* >= 2; 1 = the scalar head's logit s, read as logits [0, s] */

@@ -200,7 +200,9 @@ __global__ __launch_bounds__(128) void pref_pairs_kernel(const double* __restric
   if (threadIdx.x == 0) {
     const double m = margin_of(both, ref, pair, beta);
     const double tail = log1p(exp(-fabs(m)));
-    loss[pair] = (float)((1.0 - (double)eps) * (fmax(-m, 0.0) + tail) + (double)eps * (fmax(m, 0.0) + tail));
+    // (a weight of 0 drops its term: an action of probability 0 makes m infinite)
+    const double sure = (1.0 - (double)eps) * (fmax(-m, 0.0) + tail), other = (double)eps * (fmax(m, 0.0) + tail);
+    loss[pair] = (float)(eps == 0.f ? sure : eps == 1.f ? other : sure + other);
   }
 }
 
@@ -285,6 +287,9 @@ int lanes_for(int k) {
   return w;
 }
 
+// Rows of a launch: a grid holds fewer than 2^32 threads, 256 of a wide row.
+constexpr int64_t kRowsPerLaunch = 1 << 23;
+
 template <class T>
 hipError_t rows(const T* z, int64_t ld, int k, const int32_t* act, int64_t row0, int64_t n, float* lse, double* picked,
                 hipStream_t s) {
@@ -321,8 +326,13 @@ hipError_t launch_pref_offsets(int32_t* dst, const PrefOffsets& a, hipStream_t s
 }
 hipError_t launch_pref_rows(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
                             int64_t n, float* row_lse, double* picked, hipStream_t s) {
-  return bf ? rows((const bf16*)logits, ld, k, act, row0, n, row_lse, picked, s)
-            : rows((const float*)logits, ld, k, act, row0, n, row_lse, picked, s);
+  hipError_t e = hipSuccess;
+  for (int64_t r = 0; r < n && e == hipSuccess; r += kRowsPerLaunch) {
+    const int64_t m = n - r < kRowsPerLaunch ? n - r : kRowsPerLaunch;
+    e = bf ? rows((const bf16*)logits, ld, k, act, row0 + r, m, row_lse, picked + r, s)
+           : rows((const float*)logits, ld, k, act, row0 + r, m, row_lse, picked + r, s);
+  }
+  return e;
 }
 hipError_t launch_pref_pairs(const double* picked, const int32_t* offs, int32_t n_pairs, const float* ref, float beta,
                              float eps, float* logp, float* loss, hipStream_t s) {
@@ -337,8 +347,13 @@ hipError_t launch_pref_coef(const int32_t* offs, int32_t n_pairs, const float* r
 hipError_t launch_pref_grad(bool bf, const void* logits, int64_t ld, int32_t k, const int32_t* act, int64_t row0,
                             int64_t n, const float* row_lse, const float* coef, void* dlogits, int64_t ldd,
                             hipStream_t s) {
-  return bf ? grad((const bf16*)logits, ld, k, act, row0, n, row_lse, coef, (bf16*)dlogits, ldd, s)
-            : grad((const float*)logits, ld, k, act, row0, n, row_lse, coef, (float*)dlogits, ldd, s);
+  hipError_t e = hipSuccess;
+  for (int64_t r = 0; r < n && e == hipSuccess; r += kRowsPerLaunch) {
+    const int64_t m = n - r < kRowsPerLaunch ? n - r : kRowsPerLaunch;
+    e = bf ? grad((const bf16*)logits, ld, k, act, row0 + r, m, row_lse, coef + r, (bf16*)dlogits, ldd, s)
+           : grad((const float*)logits, ld, k, act, row0 + r, m, row_lse, coef + r, (float*)dlogits, ldd, s);
+  }
+  return e;
 }
 
 }  // namespace tx

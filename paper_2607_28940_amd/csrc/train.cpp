@@ -22,6 +22,7 @@ using namespace tx;
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff - 4096;
+constexpr int64_t kMaxGrid = 0xffffffffll / 256;  // blocks of 256 threads in a launch
 // How a launch is cut into blocks (256 CUs). Narrow blocks below kWideGrid wide
 // ones: 1000 causal tokens of 8 heads (64 wide blocks) forward 48 -> 17 us, dq 50
 // -> 26, dk and dv 52 -> 25; 4096 (256) 100 -> 86, 127 -> 112, 149 -> 137; 17 k
@@ -109,6 +110,24 @@ int check_rows(const tx_rows* t, const char* what, int es, int64_t heads, int dh
     if (!heads_in_row && !rows_in_head) return fail(TX_E_INVALID, "%s: its rows or heads overlap", what);
   }
   *dst = HeadRows{(char*)t->data, t->row_stride * es, t->head_stride * es};
+  return TX_OK;
+}
+
+// Where a tensor is written, nothing else begins (what else overlaps is the caller's to avoid).
+int check_apart(const TrainArgs& a, int64_t rows_q, int64_t rows_k, bool backward) {
+  const struct {
+    const HeadRows* t;
+    const char* name;
+    int64_t rows;
+    bool out;
+  } all[] = {{&a.q, "q", rows_q, false},         {&a.k, "k", rows_k, false},       {&a.v, "v", rows_k, false},
+             {&a.o, "out", rows_q, !backward},   {&a.dO, "d_out", rows_q, false},  {&a.dq, "d_q", rows_q, true},
+             {&a.dk, "d_k", rows_k, true},       {&a.dv, "d_v", rows_k, true}};
+  const int n = backward ? 8 : 4;
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; all[i].out && j < n; ++j)
+      if (i != j && all[i].rows && all[j].rows && all[i].t->p == all[j].t->p)
+        return fail(TX_E_INVALID, "%s is written and begins where %s does", all[i].name, all[j].name);
   return TX_OK;
 }
 
@@ -310,11 +329,13 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   if (p.rows_q > 0 && (!x.lse || ((uintptr_t)x.lse & 3))) return fail(TX_E_INVALID, "lse is null or misaligned");
   if (x.lse_stride < p.end_q)
     return fail(TX_E_INVALID, "lse stride %lld below %lld rows", (long long)x.lse_stride, (long long)p.end_q);
-  if (std::max(p.units_q, p.units_k) * H > 0x7fffffff || std::max(p.slots_q, p.slots_k) > 0x7fffffff)
-    return fail(TX_E_UNSUPPORTED, "%lld blocks in one launch", (long long)(std::max(p.units_q, p.units_k) * H));
+  if (std::max(p.units_q * H, p.units_k * G) > kMaxGrid)
+    return fail(TX_E_UNSUPPORTED, "%lld blocks in one launch", (long long)std::max(p.units_q * H, p.units_k * G));
+  if ((int64_t)H * R > 65535 * 256) return fail(TX_E_UNSUPPORTED, "%d heads of %d buckets", H, R);
   const bool drel = rel && backward && R > 0;
   if (p.rows_q == 0 && (!backward || p.rows_k == 0) && !drel) return TX_OK;
   TX_CHECK(check_ws(ws, ws_bytes, p.bytes));
+  TX_CHECK(check_apart(a, p.rows_q, p.rows_k, backward));
   TX_CHECK(check_stream(st));
 
   char* const w = (char*)ws;
@@ -373,7 +394,8 @@ int check_pref(const tx_preference_config* c, int32_t n, const int64_t* off) {
   if (c->n_actions < 1) return fail(TX_E_INVALID, "n_actions %d", c->n_actions);
   if (!std::isfinite(c->beta)) return fail(TX_E_INVALID, "beta is not finite");
   if (!(c->smoothing >= 0.f && c->smoothing <= 1.f)) return fail(TX_E_INVALID, "smoothing outside 0 .. 1");
-  if (n < 0 || n > (1 << 29)) return fail(TX_E_INVALID, "n_pairs %d", n);
+  if (n < 0) return fail(TX_E_INVALID, "n_pairs %d", n);
+  if (n > (1 << 24)) return fail(TX_E_UNSUPPORTED, "n_pairs %d above %d", n, 1 << 24);
   return check_offsets(off, 2 * (int64_t)n, "answer");
 }
 
@@ -552,6 +574,7 @@ int tx_preference_backward(const tx_preference_config* cfg, int32_t n, const int
     if (d_row_stride < cfg->n_actions || d_row_stride > ((int64_t)1 << 60) / (p.row0 + p.rows))
       return fail(TX_E_INVALID, "d_logits row stride %lld", (long long)d_row_stride);
     TX_CHECK(check_ws(ws, ws_bytes, p.bytes));
+    if (d_logits == logits) return fail(TX_E_INVALID, "d_logits is written and begins where logits do");
     TX_CHECK(check_stream(st));
     TX_HIP(put_answer_offsets((int32_t*)ws, off, 2 * (int64_t)n, st));
     float* const coef = (float*)((char*)ws + p.at_row);

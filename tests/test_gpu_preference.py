@@ -197,3 +197,59 @@ def test_differences_of_long_answers():
     # a row's sum of exponentials: 12 terms a thread and their joins, 32 u32 of it at most; rows err
     # independently, so the margin by sqrt(2 n) rows' errors
     assert abs(float(loss[0].cpu().double() - want)) < 32 * U32 * np.sqrt(2 * n) + 8 * U32 * (1 + float(want))
+
+
+@pytest.mark.parametrize("k", [3, 100])
+def test_answers_of_probability_zero(k):
+    """A masked action in one answer: log p -inf, margin infinite; a smoothing
+    of 0 or 1 leaves out the term whose weight is 0, and the gradients are finite."""
+    gen = torch.Generator().manual_seed(k)
+    z = torch.randn(4, k, generator=gen)
+    z[1, 0] = -float("inf")
+    off, one = _off([1, 1, 1, 1]), torch.ones(2)
+    for masked, eps, loss0 in ((1, 0.0, 0.0), (0, 0.0, np.inf), (1, 1.0, np.inf), (0, 1.0, 0.0)):
+        zz = z if masked else z[[1, 0, 2, 3]]
+        act = torch.zeros(4, dtype=torch.int32)
+        loss, logp, row_lse = T.preference_loss(zz.cuda(), act.cuda(), off, None, beta=0.7, smoothing=eps)
+        assert float(loss[0]) == loss0 and np.isfinite(float(loss[1])) and float(logp[masked]) == -np.inf
+        dz = T.preference_loss_backward(one.cuda(), zz.cuda(), act.cuda(), off, None, logp, row_lse, beta=0.7,
+                                        smoothing=eps).cpu().double()
+        # d loss / d m at m = +-inf: 0 where the loss is 0, else -+1, times beta and one-hot minus softmax
+        s = 0.0 if loss0 == 0.0 else -0.7 if eps == 0.0 else 0.7
+        p = torch.softmax(zz.double(), 1)
+        hot = torch.zeros(k, dtype=torch.float64)
+        hot[0] = 1.0
+        want = torch.stack([s * (hot - p[0]), -s * (hot - p[1])])
+        assert float((dz[:2] - want).abs().max()) <= 0.7 * (16 * U32 * (float(z[2:].abs().max()) + np.log(k) + 1) + 16 * U32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_rows_than_a_launch_takes(dtype):
+    """Rows are taken 2^23 at a time; the later pieces against the formula."""
+    n, k = (1 << 23) + 777, 3
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn(n, k, generator=gen, device="cuda").to(DT[dtype])
+    act = torch.randint(0, k, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    off = np.array([0, 5, (1 << 23) - 3, (1 << 23) + 100, n], dtype=np.int64)
+    loss, logp, row_lse = T.preference_loss(z, act, off, None, beta=1e-6)
+    zd = z.double()
+    lse = torch.logsumexp(zd, 1)
+    row = zd.gather(1, act.long()[:, None])[:, 0] - lse
+    size = 16 * U32 * (float(z.abs().max()) + np.log(k) + 1)
+    assert float((row_lse.double() - lse).abs().max()) <= size
+    for i in range(4):
+        want = float(row[off[i]:off[i + 1]].sum())
+        assert abs(float(logp[i]) - want) <= size * (off[i + 1] - off[i]) + 2 * U32 * abs(want)
+    dz = T.preference_loss_backward(torch.ones(2, device="cuda"), z, act, off, None, logp, row_lse, beta=1e-6)
+    u = torch.finfo(DT[dtype]).eps / 2
+    for p in (0, 1):
+        m = 1e-6 * float(row[off[2 * p]:off[2 * p + 1]].sum() - row[off[2 * p + 1]:off[2 * p + 2]].sum())
+        slope = -1e-6 / (1 + np.exp(m))
+        for a, sign in ((2 * p, 1), (2 * p + 1, -1)):
+            r = slice(int(off[a]), int(off[a + 1]))
+            hot = torch.nn.functional.one_hot(act[r].long(), k)
+            want = sign * slope * (hot - torch.exp(zd[r] - lse[r][:, None]))
+            # the margin is off by 1e-6 of the two sums' bounds, a quarter of which the slope takes
+            m_b = 1e-6 * (size * n + 4 * U32 * abs(float(row.sum())))
+            bound = 1e-6 * (m_b / 4 + size + 16 * U32) + u * want.abs()
+            assert bool(((dz[r].double() - want).abs() <= bound).all())

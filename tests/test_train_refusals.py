@@ -148,3 +148,40 @@ def test_python_arguments():
                   ([0, 4], [1, 1], [0, 4], [4])):
         with pytest.raises(T.TxError):
             T.event_attention(q, q, q, *where)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_written_tensors_begin_apart(L, backward):
+    at = {n: A + (i << 32) for i, n in enumerate(("q", "k", "v", "out", "dq", "dk", "dv"))}
+    heads = lambda n: 2 if n in ("k", "v", "dk", "dv") else 4
+    names = list(at) if backward else list(at)[:4]
+    for w in ("dq", "dk", "dv") if backward else ("out",):
+        for other in names:
+            if other == w:
+                continue
+            t = {n: _rows(heads(n), data=at[other] if n == w else at[n]) for n in names}
+            assert _rel(L, backward, **t) == T.TX_E_INVALID, (w, other)
+            assert b"begins where" in L.tx_last_error()
+    if backward:
+        assert _pref(L, True) == T.TX_E_INVALID and b"begins where" in L.tx_last_error()
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_calls_past_one_grid(L, backward):
+    U = T.TX_E_UNSUPPORTED
+    big = dict(q=_rows(65536, 32), out=_rows(65536, 32), k=_rows(1, 32), v=_rows(1, 32))
+    if backward:
+        big.update(dq=_rows(65536, 32), dk=_rows(1, 32), dv=_rows(1, 32))
+    n = 300
+    c = _cfg(H=65536, G=1, dh=32, R=0)
+    if backward:  # (d_out of the helper has 4 heads of 64: rows that overlap may be read)
+        assert _rel(L, True, cfg=c, off=np.arange(n + 1), lse_stride=n, **big) == U
+    else:
+        assert _rel(L, False, cfg=c, off=np.arange(n + 1), lse_stride=n, **big) == U
+    assert b"one launch" in L.tx_last_error()
+    c = _cfg(H=65536, G=1, dh=32, R=512)
+    assert _rel(L, backward, cfg=c, off=(0, 5, 9), **big) == U and b"buckets" in L.tx_last_error()
+    p = T.PreferenceConfig(T.TX_F32, 4, 0.1, 0.0)
+    off = T._i64([0, 2, 5])
+    assert L.tx_preference_workspace_bytes(ctypes.byref(p), (1 << 24) + 1, T._p(off, T.I64P)) == 0
+    assert b"n_pairs" in L.tx_last_error()
