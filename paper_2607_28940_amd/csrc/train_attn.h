@@ -269,11 +269,14 @@ struct Wave {
     for (int c = 0; c < G::NC; ++c) a = rows_mma(row_frag(tile, rb, c), f[c], a);
     if constexpr (BF && G::NC >= 4) pace<G::NC, 1, 1>();
   }
+  // (the second added to what a2 holds)
+  template <int FIRST = 0>
   __device__ __forceinline__ void rows_products(const lds_char* t1, const u32x4_t (&f1)[G::NC], floatx16& a1,
                                                 const lds_char* t2, const u32x4_t (&f2)[G::NC], floatx16& a2,
                                                 int rb) const {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) a1[v] = 0.f, a2[v] = 0.f;
+    for (int v = 0; v < 16; ++v) a1[v] = 0.f;
+    if constexpr (BF && FIRST > 0) __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
 #pragma unroll
     for (int c = 0; c < G::NC; ++c) {
       a1 = rows_mma(row_frag(t1, rb, c), f1[c], a1);
@@ -287,7 +290,8 @@ struct Wave {
                                                     const lds_char* t2, const lds_char* t3, floatx16& a2,
                                                     int rb) const {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) a1[v] = 0.f, a2[v] = 0.f;
+    for (int v = 0; v < 16; ++v) a1[v] = 0.f;
+    if constexpr (BF) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
     for (int c = 0; c < G::NC; ++c) {
       a1 = rows_mma(row_frag(t1, rb, c), f1[c], a1);

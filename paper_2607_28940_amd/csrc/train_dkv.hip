@@ -103,15 +103,18 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
     if (!REL && id >= QT) p = (const float2_t*)(a.row_lim + (r & ~1));
     return *p;
   };
-  auto park_stat = [&](float2_t x, int t, int b) {
+  // in the form that the tiles of the class take: plain ones the negative lse and
+  // their bias together, both minus D, which dP's product starts from
+  auto park_stat = [&](auto masked_c, float2_t x, int t, int b) {
     int id = NARROW ? lane : tid;
     asm volatile("" : "+v"(id));
     const int r = t * QT + id % QT;
     const bool ok = r < g.nq;
     lds_float* const to = stat + b * 3 * QT + id;
     if (id < QT) {
-      to[0] = ok ? x[0] : INFINITY;  // probabilities 0
-      to[QT] = ok ? x[1] : 0.f;
+      const float ls = ok ? x[0] : INFINITY;  // (probabilities 0)
+      to[0] = decltype(masked_c)::value ? ls : far - ls;
+      to[QT] = ok ? -x[1] : 0.f;
     } else if (!REL && id < 2 * QT) {
       to[QT] = ok ? ((g.q0 + r - a.q_base) & 1 ? x[1] : x[0]) : 0.f;
     }
@@ -153,18 +156,23 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
         const int qr = t * QT + 32 * qb;  // first query of the 32
         if (MASKED && (qr >= g.nq || (REL && qr + 31 < k_wave))) continue;
         floatx16 s, p;
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+          const floatx4 nD = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) p[4 * gq + t] = nD[t];
+        }
         if constexpr (V_LDS) w.rows_products_lds(sQ, kf, s, sO, sVb + wave * 32 * Gm::RB, p, qb);
-        else w.rows_products(sQ, kf, s, sO, vf, p, qb);
+        else w.template rows_products<4>(sQ, kf, s, sO, vf, p, qb);
         if (!MASKED) {
 #pragma unroll
           for (int gq = 0; gq < 4; ++gq) {
             const floatx4 ls = *reinterpret_cast<const lds_floatx4*>(ss + 32 * qb + 8 * gq + 4 * hi);
-            const floatx4 Dv = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
               const int v = 4 * gq + t;
-              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, far - ls[t]));
-              p[v] = s[v] * (p[v] - Dv[t]);
+              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, ls[t]));
+              p[v] *= s[v];
             }
           }
           w.cols_mma2(sO, s, dv, sQ, p, dk, qb);
@@ -175,7 +183,6 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq) {
           const floatx4 ls = *reinterpret_cast<const lds_floatx4*>(ss + 32 * qb + 8 * gq + 4 * hi);
-          const floatx4 Dv = *reinterpret_cast<const lds_floatx4*>(ss + QT + 32 * qb + 8 * gq + 4 * hi);
           floatx4 lm = {0.f, 0.f, 0.f, 0.f};
           if (!REL) lm = *reinterpret_cast<const lds_floatx4*>(ss + 2 * QT + 32 * qb + 8 * gq + 4 * hi);
 #pragma unroll
@@ -186,7 +193,7 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
             vis |= see ? 1u << v : 0u;
             const float lg = fmaf(s[v], a.scale_log2, bias);
             s[v] = see ? __builtin_amdgcn_exp2f(lg - ls[t]) : 0.f;
-            p[v] = see ? s[v] * (p[v] - Dv[t]) : 0.f;
+            p[v] = see ? s[v] * p[v] : 0.f;
           }
         }
         if constexpr (STRICT) {
@@ -243,7 +250,7 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
       if (MANY ? hh >= h1 : t >= t1) return;
       int h = hk * per + hh, now = t;
       fetch(h, now, 0);
-      park_stat(fetch_stat(h, now), now, 0);
+      park_stat(masked_c, fetch_stat(h, now), now, 0);
       for (int b = 0;; b = BUFS == 2 ? b ^ 1 : 0) {
         if (NARROW) tile_ready();
         else tiles_ready();
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
         if (k_wave < g.nk) tile(masked_c, now, b);
         if (!more) break;
         if (BUFS == 1) tile_read(), fetch(h, t, 0);
-        park_stat(st, t, BUFS == 2 ? b ^ 1 : 0);
+        park_stat(masked_c, st, t, BUFS == 2 ? b ^ 1 : 0);
         now = t;
       }
       if (!NARROW) __syncthreads();

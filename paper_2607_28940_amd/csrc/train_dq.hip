@@ -28,6 +28,13 @@ constexpr int dq_lds_bytes() {
 template <class T, int DH, bool NARROW>
 constexpr int dq_blocks() { return NARROW || sizeof(T) == 4 ? 1 : DH == 128 ? 2 : DH == 64 ? 3 : 4; }
 
+// Whether dP's product starts from -D, 16 registers of it, instead of a
+// subtraction per pair: where the block's share of the registers has room (147 k
+// queries of 2.3 k keys at d_head 128: 1.86 against 1.91 ms; at 64, with three
+// blocks a CU, 121 against 114 us for 17 k queries).
+template <class T, int DH, bool REL, bool NARROW>
+constexpr bool from_d() { return sizeof(T) == 2 && !NARROW && (DH == 32 || (DH == 128 && !REL)); }
+
 // Per wave and 32 keys: S^T = K Q^T, dP^T = V dO^T (lanes = queries, so lse and
 // D are one register each), dS = P (dP - D), dQ^T += K^T dS^T with dS^T taken
 // from the accumulators. dS is rounded to bf16 for that product (relative 2^-9
@@ -71,6 +78,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
   using W = Wave<T, DH>;
   constexpr int KT = key_tile<T, NARROW>(), KB = KT / 32, TB = dq_tile_bytes<T, DH, NARROW>();
   constexpr int BUFS = dq_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows;
+  constexpr bool FROM_D = from_d<T, DH, REL, NARROW>();
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
   lds_float* const tab = (lds_float*)(smem + dq_lds_bytes<T, DH, NARROW>());
@@ -184,6 +192,10 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
       for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
     if (sums)
       for (int i = tid; i < 4 * entries; i += 256) sub[i] = 0.f;
+    floatx16 from;  // FROM_D: what dP's product starts from
+    if constexpr (FROM_D)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) from[v] = -D;
     bool again = false;
     auto tile = [&](auto masked_c, int t, int b) {
       constexpr bool MASKED = decltype(masked_c)::value;
@@ -195,10 +207,14 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         floatx16 s, p;
+        if constexpr (FROM_D) p = from;
+        else
+#pragma unroll
+          for (int v = 0; v < 16; ++v) p[v] = 0.f;
         w.rows_products(sK, qf, s, sV, df, p, kb);
         if (!MASKED) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (p[v] - D);
+          for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (FROM_D ? p[v] : p[v] - D);
           w.cols_mma(sK, kb, s, dq);
           continue;
         }
@@ -211,7 +227,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
           vis |= see ? 1u << v : 0u;
           // in two steps: a large bias rounds the logit as it did in the forward
           const float lg = fmaf(s[v], a.scale_log2, bias);
-          s[v] = see ? __builtin_amdgcn_exp2f(lg - lse2) * (p[v] - D) : 0.f;
+          s[v] = see ? __builtin_amdgcn_exp2f(lg - lse2) * (FROM_D ? p[v] : p[v] - D) : 0.f;
         }
         if (sums) {
           // lane d (or 64 + d): distance q_wave - k0 - 32 kb + d; past the padding nothing is kept
@@ -247,6 +263,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
     if (NARROW) __syncthreads();  // (the bias table and the sums)
     if (t < t_end) fetch(t, 0);
     pin(qf), pin(df), pin(lim), pin(lse2), pin(D);
+    if constexpr (FROM_D) pin(from);
     ready();
     run(std::false_type{}, t_plain, q_wave < g.nq);
     run(std::true_type{}, t_end, true);
