@@ -34,6 +34,13 @@ constexpr int64_t kMaxGrid = 0xffffffffll / 256;  // blocks of 256 threads in a 
 // and the join reads costs more than it saves (4096 tokens 86 -> 131 us towards
 // 1024 blocks, 1000 tokens 17 -> 31 us at 2 tiles a part).
 constexpr int64_t kWideGrid = 512, kFullGrid = 512;
+// Shared key heads: with a full card packed blocks throughout (few rows of 32
+// users, 16 heads on 4: 94 -> 83 us forward, 111 -> 97 dq). With less, packed ones
+// read the keys a quarter as often but run a chain of tiles four times as long: of
+// 4 heads at d_head 64 and less from 4096 keys on (3 users of 8192, 45 rows each:
+// 53 -> 43 us; of 1024: 14 -> 24); two heads (8192: 48 us both) and d_head 128, half
+// as many blocks a CU (49 -> 59), do not gain.
+constexpr int kPackKeys = 4096;
 constexpr int kMaxParts = 64, kMinSteps = 4, kMinStepsF32 = 2;
 
 // Metadata goes up as kernel arguments, 3 KB a launch: no staging buffer whose
@@ -135,7 +142,8 @@ int check_apart(const TrainArgs& a, int64_t rows_q, int64_t rows_k, bool backwar
 struct AttnPlan {
   std::vector<TrainGroup> groups;
   std::vector<int32_t> ev_row, ev_prefix;  // event form
-  int q_rows = kWideRows, k_rows = kWideRows;
+  int q_rows = kWideRows, k_rows = kWideRows, pack = 0;
+  bool q_narrow = false, k_narrow = false;
   int64_t units_q = 0, units_k = 0, tiles = 0, slots_q = 0, slots_k = 0;
   double pairs = 0;                        // visible (query, key) pairs
   int64_t rows_q = 0, rows_k = 0;          // rows of the call
@@ -180,26 +188,36 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   }
   // wide blocks where they would fill the card, narrow ones otherwise
   int64_t wide_q = 0, wide_k = 0;
-  for (const TrainGroup& g : p.groups) wide_q += blocks_of(g.nq) * H, wide_k += blocks_of(g.nk) * G;
-  p.q_rows = wide_q >= kWideGrid ? kWideRows : kNarrowRows;
-  p.k_rows = wide_k >= kWideGrid ? kWideRows : kNarrowRows;
+  double pairs_of_rows = 0;
+  for (size_t i = 0; i < p.groups.size(); ++i) {
+    const TrainGroup& g = p.groups[i];
+    wide_q += blocks_of(g.nq) * H, wide_k += blocks_of(g.nk) * G;
+    pairs_of_rows += (double)g.nq * keys[i];
+  }
+  const int per = H / G;
+  p.pack = rel ? 0 : per % 4 == 0 ? 2 : per % 2 == 0 ? 1 : 0;
+  if (wide_q < kWideGrid && !(p.pack == 2 && dh <= 64 && pairs_of_rows >= kPackKeys * (double)p.rows_q)) p.pack = 0;
+  p.q_narrow = !p.pack && wide_q < kWideGrid;
+  p.k_narrow = wide_k < kWideGrid;
   // a narrow block's tiles (128 KB at d_head 128) leave room for the bias sums of
   // some 1300 buckets
-  if (backward && rel && train_dq_lds(c.dtype == TX_BF16, dh, c.rel_pos_buckets, p.q_rows) > kTrainMaxLds)
-    p.q_rows = kWideRows;
+  if (backward && rel && train_dq_lds(c.dtype == TX_BF16, dh, c.rel_pos_buckets, p.q_narrow) > kTrainMaxLds)
+    p.q_narrow = false;
+  p.q_rows = p.q_narrow ? kNarrowRows : kWideRows >> p.pack;
+  p.k_rows = p.k_narrow ? kNarrowRows : kWideRows;
   int64_t steps_q = 0, steps_k = 0;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     const TrainGroup& g = p.groups[i];
     const double share = rel ? 0.5 : 1.0;  // a causal block covers half of the group's tiles on average
-    steps_q += (int64_t)std::ceil(blocks_of(g.nq, p.q_rows) * tiles_of(keys[i]) * share) * H;
+    steps_q += (int64_t)std::ceil(blocks_of(g.nq, p.q_rows) * tiles_of(keys[i]) * share) * (H >> p.pack);
     steps_k += (int64_t)std::ceil(blocks_of(g.nk, p.k_rows) * tiles_of(g.nq) * (H / G) * share) * G;
   }
   const int min_steps = c.dtype == TX_F32 ? kMinStepsF32 : kMinSteps;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     TrainGroup& g = p.groups[i];
     const int64_t bq = blocks_of(g.nq, p.q_rows), bk = blocks_of(g.nk, p.k_rows);
-    const int nq_steps = p.q_rows == kNarrowRows ? 4 * min_steps : min_steps,
-              nk_steps = p.k_rows == kNarrowRows ? 4 * min_steps : min_steps;
+    const int nq_steps = p.q_narrow ? 4 * min_steps : min_steps,
+              nk_steps = p.k_narrow ? 4 * min_steps : min_steps;
     g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, nq_steps) : 1;
     g.unit_q = (int32_t)p.units_q;
     g.slot_q = (int32_t)p.slots_q;
@@ -349,7 +367,6 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
     TX_HIP(put_all(w, p.meta, st));
   a.groups = (const TrainGroup*)w;
   a.n_groups = (int32_t)p.groups.size();
-  a.n_units = (int32_t)p.units_q;
   a.H = H, a.G = G;
   a.lse = x.lse;
   a.lse_ld = x.lse_stride;
@@ -364,6 +381,11 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   a.scale_log2 = (float)(a.scale * 1.4426950408889634);
   a.partial = (float*)(w + p.at.partial);
   a.q_rows = p.q_rows, a.k_rows = p.k_rows;
+  a.q_narrow = p.q_narrow, a.k_narrow = p.k_narrow;
+  a.pack = p.pack;
+  a.n_units = (int32_t)p.units_q, a.k_units = (int32_t)p.units_k;
+  a.q_chunk = place_chunk(p.units_q, H >> p.pack);
+  a.k_chunk = place_chunk(p.units_k, G);
   a.drel_part = (float*)(w + p.at.drel);
   if (limits && !in_one)
     TX_HIP(launch_train_limits(a.groups, a.n_groups, (int32_t)p.tiles, (const int32_t*)(w + p.o_row),
@@ -381,8 +403,8 @@ int run_attn(const tx_attn_config& c, bool backward, bool rel, const AttnPlan& p
   if (drel) TX_LAUNCH(K_TRAIN_DQ, 0, 0, launch_train_drel(bf, a, (float*)(w + p.at.drel2), x.d_rel, st));
   if (p.units_k)
     TX_LAUNCH(K_TRAIN_DKV, 4 * prod, 2 * qb + 4 * kb + 2 * stat,
-              launch_train_dkv(bf, dh, rel, a, (int32_t)p.units_k, st));
-  if (p.slots_k) TX_LAUNCH(K_TRAIN_DKV, 0, 0, launch_train_dkv_join(bf, dh, a, (int32_t)p.units_k, st));
+              launch_train_dkv(bf, dh, rel, a, st));
+  if (p.slots_k) TX_LAUNCH(K_TRAIN_DKV, 0, 0, launch_train_dkv_join(bf, dh, a, st));
   return TX_OK;
 }
 

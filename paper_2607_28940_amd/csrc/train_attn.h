@@ -41,7 +41,10 @@ struct TrainGroup {
 // ones give all four the same 32 rows and every fourth tile, each wave with
 // buffers of its own and no barrier between tiles, and add up at the end: for
 // calls whose wide blocks would leave most of the card idle, each with a long
-// chain of tiles.
+// chain of tiles. Where query heads share a key head (and no bias tells them
+// apart), a wide block of queries packs 2 or 4 of them: its waves take the same
+// 64 or 32 rows of several heads, so that few rows still fill it and read the
+// keys and values once.
 constexpr int kWideRows = 128, kNarrowRows = 32;
 constexpr int kTrainQTile = 64;   // granularity of the per-tile key limits
 constexpr int kTrainMaxRel = 2048;
@@ -59,7 +62,8 @@ struct HeadRows {
 
 struct TrainArgs {
   const TrainGroup* groups;
-  int32_t n_groups, n_units, H, G;  // H query heads, G key heads
+  int32_t n_groups, H, G;  // H query heads, G key heads
+  int32_t n_units, q_chunk, k_units, k_chunk;  // units of either side and their place_chunk
   HeadRows q, k, v, o, dO, dq, dk, dv;
   float* lse;           // [H][lse_ld], natural logarithm
   int64_t lse_ld;
@@ -74,6 +78,8 @@ struct TrainArgs {
   float scale, scale_log2;
   float* partial;       // slots of divided blocks
   int32_t q_rows, k_rows;   // rows of a query-side and of a key-side block
+  bool q_narrow, k_narrow;
+  int32_t pack;             // log2 of the query heads in a wide query-side block
   float* drel_part;     // [unit][H][R] sums of dS by bucket
 };
 
@@ -81,8 +87,8 @@ hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipSt
 hipError_t launch_train_fwd_join(bool bf, int dh, const TrainArgs& a, hipStream_t s);
 hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
 hipError_t launch_train_dq_join(bool bf, int dh, const TrainArgs& a, hipStream_t s);
-hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
-hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, int32_t n_units_k, hipStream_t s);
+hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s);
+hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, hipStream_t s);
 // drel[h][b] from the units' sums; scratch: [chunks][H][R] floats, chunks = ceil(units / 32)
 hipError_t launch_train_drel(bool bf, const TrainArgs& a, float* scratch, void* drel, hipStream_t s);
 // row_lim and tile_lim of the event form (n_tiles > 0) from the groups and the
@@ -95,6 +101,25 @@ hipError_t launch_train_put_limits(void* dst, const void* meta, size_t bytes, in
                                    size_t o_row, size_t o_prefix, int32_t* row_lim, int32_t q_base, TileLim* tile_lim,
                                    hipStream_t s);
 
+// Blocks go to the card's 8 XCDs in turn, each with an L2 of its own, and the
+// units of a group read the same rows of the other side. With a multiple of 8
+// heads (or packed heads) a launch runs over the heads first, so that a head
+// stays on one XCD. With 1, 2 or 4 an XCD gets one head and up to 32 units in a
+// row of it, then skips what the XCDs of the same head take: dk and dv of 147 k
+// queries of 2.3 k keys, 8 heads on 2 key heads: 4.48 -> 3.50 ms. Other counts run over the
+// heads first as well.
+__host__ __device__ inline bool placed(int heads) { return heads == 1 || heads == 2 || heads == 4; }
+inline int place_chunk(int64_t units, int heads) {
+  if (!placed(heads) || units == 0) return 0;
+  const int64_t xcds = 8 / heads, rounds = (units + 32 * xcds - 1) / (32 * xcds);
+  return (int)((units + xcds * rounds - 1) / (xcds * rounds));
+}
+inline unsigned place_grid(int64_t units, int heads, int chunk) {
+  if (!chunk) return (unsigned)(units * heads);
+  const int64_t round = (int64_t)chunk * (8 / heads);
+  return (unsigned)((units + round - 1) / round * round * heads);
+}
+
 // floats of one partial slot
 __host__ __device__ inline size_t train_fwd_slot(int rows, int dh) { return (size_t)rows * (dh + 2); }
 __host__ __device__ inline size_t train_dq_slot(int rows, int dh) { return (size_t)rows * dh; }
@@ -102,7 +127,7 @@ __host__ __device__ inline size_t train_dkv_slot(int rows, int dh) { return (siz
 
 // LDS of a block of the dq kernel: its tiles and the bias tables of R buckets;
 // what a CU has for one block, less the compiler's own.
-size_t train_dq_lds(bool bf, int dh, int R, int rows);
+size_t train_dq_lds(bool bf, int dh, int R, bool narrow);
 constexpr size_t kTrainMaxLds = 159 * 1024;
 
 #ifdef __HIPCC__
@@ -649,6 +674,19 @@ __device__ __forceinline__ float bias_value(const T* __restrict__ rel, int R, in
 template <class T>
 __device__ __forceinline__ void stage_bias(lds_float* tab, const T* __restrict__ rel, int R, int h, int tid) {
   for (int i = tid; i < bias_entries(R); i += 256) tab[i] = bias_value(rel, R, h, i - kBiasPad);
+}
+
+// The block's unit and head (see placed()); a unit past the last one has no work.
+__device__ __forceinline__ void place(int chunk, int heads, int& unit, int& head) {
+  const int b = blockIdx.x;
+  if (chunk) {
+    const int i = b >> 3, x = b & 7;
+    head = x & (heads - 1);
+    unit = (i / chunk * (8 / heads) + x / heads) * chunk + i % chunk;
+  } else {
+    head = b % heads;
+    unit = b / heads;
+  }
 }
 
 // Lets a kernel use more than 64 KB of LDS a block: remembers the most that it

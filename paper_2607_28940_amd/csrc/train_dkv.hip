@@ -57,7 +57,10 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
   lds_float* const stats = (lds_float*)(smem + dkv_lds_bytes<T, DH, NARROW>());
   lds_float* const tab = stats + stat_floats<T, DH, NARROW>();
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int unit = blockIdx.x / a.G, hk = blockIdx.x % a.G, per = a.H / a.G;
+  int unit, hk;
+  place(a.k_chunk, a.G, unit, hk);
+  if (unit >= a.k_units) return;
+  const int per = a.H / a.G;
   const TrainGroup g = a.groups[find_group<true>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_k, local = unit - g.unit_k, part = local % parts, kblk = local / parts;
   const int k_first = kblk * ROWS, k_wave = k_first + (NARROW ? 0 : wave * 32), key = k_wave + l32;
@@ -346,28 +349,28 @@ __global__ __launch_bounds__(256) void train_dkv_join_kernel(const TrainArgs a) 
 }
 
 template <class T, int DH, bool REL, bool NARROW>
-hipError_t dkv_launch(const TrainArgs& a, int32_t n_units, hipStream_t s) {
+hipError_t dkv_launch(const TrainArgs& a, hipStream_t s) {
   const size_t lds = dkv_lds_bytes<T, DH, NARROW>() + 4 * stat_floats<T, DH, NARROW>() +
                      (REL ? 4 * (size_t)bias_entries(a.R) : 0);
   static LdsAllowed so_far;
   const hipError_t e = allow_lds((const void*)train_dkv_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
-  train_dkv_kernel<T, DH, REL, NARROW><<<dim3((unsigned)n_units * a.G), 256, lds, s>>>(a);
+  train_dkv_kernel<T, DH, REL, NARROW><<<place_grid(a.k_units, a.G, a.k_chunk), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 template <class T, int DH>
-hipError_t dkv_join(const TrainArgs& a, int32_t n_units, hipStream_t s) {
-  train_dkv_join_kernel<T, DH><<<dim3((unsigned)n_units * a.G), 256, 0, s>>>(a);
+hipError_t dkv_join(const TrainArgs& a, hipStream_t s) {
+  train_dkv_join_kernel<T, DH><<<dim3((unsigned)a.k_units * a.G), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32_t n, hipStream_t s) {
-  const bool narrow = a.k_rows == kNarrowRows;
+hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
+  const bool narrow = a.k_narrow;
 #define TX_CASE(T, D)                                                                                       \
-  return narrow ? (rel ? dkv_launch<T, D, true, true>(a, n, s) : dkv_launch<T, D, false, true>(a, n, s))    \
-                : (rel ? dkv_launch<T, D, true, false>(a, n, s) : dkv_launch<T, D, false, false>(a, n, s))
+  return narrow ? (rel ? dkv_launch<T, D, true, true>(a, s) : dkv_launch<T, D, false, true>(a, s))    \
+                : (rel ? dkv_launch<T, D, true, false>(a, s) : dkv_launch<T, D, false, false>(a, s))
   if (bf) {
     if (dh == 32) TX_CASE(bf16, 32);
     if (dh == 64) TX_CASE(bf16, 64);
@@ -379,10 +382,10 @@ hipError_t launch_train_dkv(bool bf, int dh, bool rel, const TrainArgs& a, int32
 #undef TX_CASE
 }
 
-hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, int32_t n, hipStream_t s) {
+hipError_t launch_train_dkv_join(bool bf, int dh, const TrainArgs& a, hipStream_t s) {
   if (bf)
-    return dh == 32 ? dkv_join<bf16, 32>(a, n, s) : dh == 64 ? dkv_join<bf16, 64>(a, n, s) : dkv_join<bf16, 128>(a, n, s);
-  return dh == 32 ? dkv_join<float, 32>(a, n, s) : dh == 64 ? dkv_join<float, 64>(a, n, s) : dkv_join<float, 128>(a, n, s);
+    return dh == 32 ? dkv_join<bf16, 32>(a, s) : dh == 64 ? dkv_join<bf16, 64>(a, s) : dkv_join<bf16, 128>(a, s);
+  return dh == 32 ? dkv_join<float, 32>(a, s) : dh == 64 ? dkv_join<float, 64>(a, s) : dkv_join<float, 128>(a, s);
 }
 
 }  // namespace tx

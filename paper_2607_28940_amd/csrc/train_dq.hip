@@ -77,19 +77,25 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
   constexpr int KT = key_tile<T, NARROW>(), KB = KT / 32, TB = dq_tile_bytes<T, DH, NARROW>();
-  constexpr int BUFS = dq_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows;
+  constexpr int BUFS = dq_buffers<T, DH, NARROW>();
   constexpr bool FROM_D = from_d<T, DH, REL, NARROW>();
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
   lds_float* const tab = (lds_float*)(smem + dq_lds_bytes<T, DH, NARROW>());
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  // a wide block's waves: 4 >> pack of them on the rows of each of its heads
+  const int pack = NARROW || REL ? 0 : a.pack, ROWS = NARROW ? kNarrowRows : kWideRows >> pack;
+  int unit, h0;
+  place(a.q_chunk, a.H >> pack, unit, h0);
+  if (unit >= a.n_units) return;
+  h0 <<= pack;
+  const int h = h0 + (wave >> (2 - pack)), w_row = NARROW ? 0 : 32 * (wave & ((4 >> pack) - 1));
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_q, blocks = (g.nq + ROWS - 1) / ROWS;
   const int local = unit - g.unit_q, part = local % parts;
   const int qb = blocks - 1 - local / parts;
   const int q_first = qb * ROWS;
-  const int hk = h / (a.H / a.G);
+  const int hk = h0 / (a.H / a.G);
   const int R = REL ? a.R : 0, R1 = max(R, 1) - 1, entries = bias_entries(R);
   const bool sums = REL && R > 1;
   lds_float* const sub = tab + entries;
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
   } else {
     const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     k_end = tl[0].hi;
-    if (!NARROW && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+    if (ROWS > kTrainQTile && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
   const float far = REL ? bias_value((const T*)a.rel, R, h, R1) : 0.f;
@@ -113,7 +119,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
   } else {
     const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     t_plain = tl[0].lo;
-    if (!NARROW && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    if (ROWS > kTrainQTile && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
     t_plain /= KT;
   }
   if (parts > 1) {
@@ -123,7 +129,7 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
   }
   t_plain = min(t_plain, t_end);
 
-  const int q_wave = q_first + (NARROW ? 0 : wave * 32), q_row = q_wave + l32;
+  const int q_wave = q_first + w_row, q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
   const int64_t row = g.q0 + q_row;
   float D = 0.f;
@@ -293,11 +299,11 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
     return;
   }
   if (slot) {
-    if (exists) store_partial<T, DH>(dq, slot + (size_t)(wave * 32 + l32) * DH, hi);
+    if (exists) store_partial<T, DH>(dq, slot + (size_t)(w_row + l32) * DH, hi);
     return;
   }
   if (q_wave < g.nq)
-    store_rows<T, DH>(dq, a.scale, smem + wave * 32 * Gm::RB, out + wave * 32 * a.dq.row, a.dq.row, g.nq - q_wave, lane);
+    store_rows<T, DH>(dq, a.scale, smem + wave * 32 * Gm::RB, out + w_row * a.dq.row, a.dq.row, g.nq - q_wave, lane);
 }
 
 template <class T, int DH>
@@ -356,7 +362,7 @@ hipError_t dq_launch(const TrainArgs& a, hipStream_t s) {
   static LdsAllowed so_far;
   const hipError_t e = allow_lds((const void*)train_dq_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
-  train_dq_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  train_dq_kernel<T, DH, REL, NARROW><<<place_grid(a.n_units, a.H >> a.pack, a.q_chunk), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 template <class T, int DH>
@@ -367,8 +373,7 @@ hipError_t dq_join(const TrainArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t train_dq_lds(bool bf, int dh, int R, int rows) {
-  const bool narrow = rows == kNarrowRows;
+size_t train_dq_lds(bool bf, int dh, int R, bool narrow) {
 #define TX_CASE(T, D) return table_bytes(R) + (narrow ? dq_lds_bytes<T, D, true>() : dq_lds_bytes<T, D, false>())
   if (bf) {
     if (dh == 32) TX_CASE(bf16, 32);
@@ -382,7 +387,7 @@ size_t train_dq_lds(bool bf, int dh, int R, int rows) {
 }
 
 hipError_t launch_train_dq(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
-  const bool narrow = a.q_rows == kNarrowRows;
+  const bool narrow = a.q_narrow;
 #define TX_CASE(T, D)                                                                               \
   return narrow ? (rel ? dq_launch<T, D, true, true>(a, s) : dq_launch<T, D, false, true>(a, s))    \
                 : (rel ? dq_launch<T, D, true, false>(a, s) : dq_launch<T, D, false, false>(a, s))

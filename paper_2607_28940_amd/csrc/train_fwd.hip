@@ -36,19 +36,25 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   using Gm = Geo<T, DH>;
   using W = Wave<T, DH>;
   constexpr int KT = key_tile<T, NARROW>(), KB = KT / 32, TB = fwd_tile_bytes<T, DH, NARROW>();
-  constexpr int BUFS = fwd_buffers<T, DH, NARROW>(), ROWS = NARROW ? kNarrowRows : kWideRows;
+  constexpr int BUFS = fwd_buffers<T, DH, NARROW>();
   extern __shared__ __align__(1024) char smem_[];
   lds_char* const smem = (lds_char*)smem_;
   lds_float* const tab = (lds_float*)(smem + fwd_lds_bytes<T, DH, NARROW>());
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int unit = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  // a wide block's waves: 4 >> pack of them on the rows of each of its heads
+  const int pack = NARROW || REL ? 0 : a.pack, ROWS = NARROW ? kNarrowRows : kWideRows >> pack;
+  int unit, h0;
+  place(a.q_chunk, a.H >> pack, unit, h0);
+  if (unit >= a.n_units) return;
+  h0 <<= pack;
+  const int h = h0 + (wave >> (2 - pack)), w_row = NARROW ? 0 : 32 * (wave & ((4 >> pack) - 1));
   const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
   const int parts = g.parts_q, blocks = (g.nq + ROWS - 1) / ROWS;
   const int local = unit - g.unit_q, part = local % parts;
   // a group's last rows see the most keys (later events have longer prefixes): first
   const int qb = blocks - 1 - local / parts;
   const int q_first = qb * ROWS;
-  const int hk = h / (a.H / a.G);
+  const int hk = h0 / (a.H / a.G);
 
   // keys that any row of the block sees, and the block's share of them
   int k_end;
@@ -57,7 +63,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   } else {
     const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     k_end = tl[0].hi;
-    if (!NARROW && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
+    if (ROWS > kTrainQTile && q_first + kTrainQTile < g.nq) k_end = max(k_end, tl[1].hi);
   }
   const int R = REL ? a.R : 0, R1 = max(R, 1) - 1;  // R1: the first distance of the last bucket
   if (REL) stage_bias(tab, (const T*)a.rel, R, h, tid);
@@ -75,7 +81,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   } else {
     const TileLim* tl = a.tile_lim + g.qt0 + q_first / kTrainQTile;
     t_plain = tl[0].lo;
-    if (!NARROW && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
+    if (ROWS > kTrainQTile && q_first + kTrainQTile < g.nq) t_plain = min(t_plain, tl[1].lo);
     t_plain /= KT;
   }
   if (parts > 1) {
@@ -85,7 +91,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   }
   t_plain = min(t_plain, t_end);
 
-  const int q_wave = q_first + (NARROW ? 0 : wave * 32);  // first query of the wave, within the group
+  const int q_wave = q_first + w_row;  // first query of the wave, within the group
   const int q_row = q_wave + l32;
   const bool exists = q_row < g.nq;
   int lim = 0;  // visible keys of the lane's query
@@ -285,7 +291,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
     return;
   }
   if (slot) {
-    const int r = wave * 32 + l32;
+    const int r = w_row + l32;
     if (exists) {
       store_partial<T, DH>(o, slot + (size_t)r * DH, hi);
       if (hi == 0) slot[ROWS * DH + r] = m, slot[ROWS * (DH + 1) + r] = l;
@@ -297,7 +303,7 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   if (exists && hi == 0)
     a.lse[(int64_t)h * a.lse_ld + g.q0 + q_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kTrainLn2;
   if (n_rows > 0)
-    store_rows<T, DH>(o, l == 0.f ? 0.f : 1.f / l, smem + wave * 32 * Gm::RB, out + wave * 32 * a.o.row, a.o.row, n_rows,
+    store_rows<T, DH>(o, l == 0.f ? 0.f : 1.f / l, smem + wave * 32 * Gm::RB, out + w_row * a.o.row, a.o.row, n_rows,
                       lane);
 }
 
@@ -424,7 +430,7 @@ hipError_t fwd(const TrainArgs& a, hipStream_t s) {
   static LdsAllowed so_far;
   const hipError_t e = allow_lds((const void*)train_fwd_kernel<T, DH, REL, NARROW>, lds, so_far);
   if (e != hipSuccess) return e;
-  train_fwd_kernel<T, DH, REL, NARROW><<<dim3((unsigned)a.n_units * a.H), 256, lds, s>>>(a);
+  train_fwd_kernel<T, DH, REL, NARROW><<<place_grid(a.n_units, a.H >> a.pack, a.q_chunk), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -437,7 +443,7 @@ hipError_t fwd_join(const TrainArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_train_fwd(bool bf, int dh, bool rel, const TrainArgs& a, hipStream_t s) {
-  const bool narrow = a.q_rows == kNarrowRows;
+  const bool narrow = a.q_narrow;
 #define TX_CASE(T, D)                                                                   \
   return narrow ? (rel ? fwd<T, D, true, true>(a, s) : fwd<T, D, false, true>(a, s))    \
                 : (rel ? fwd<T, D, true, false>(a, s) : fwd<T, D, false, false>(a, s))

@@ -200,3 +200,23 @@ def test_graphs_of_divided_blocks():
         _step(q * 2, k, v, do, where)
         torch.cuda.synchronize()
         assert all(torch.equal(first[n], res[n]) for _, res in graphs for n in first)
+
+
+FEW_ROWS = [(4500, [(33, 4500), (1, 4097)])]                         # long keys, divided blocks
+MANY = [(1 + 37 * u % 150, [(1 + 13 * u % 70, 0 if u % 9 == 0 else 1 + u % (1 + 37 * u % 150)), (u % 3, 1)])
+        for u in range(260)]
+
+
+@pytest.mark.parametrize("users", [FEW_ROWS, MANY], ids=["few_rows", "many"])
+@pytest.mark.parametrize("H,G", [(4, 2), (6, 1), (8, 1), (12, 3)])
+@pytest.mark.parametrize("dtype,dh", [("f32", 32), ("f32", 128), ("bf16", 64), ("bf16", 128)])
+def test_heads_that_share_a_block(dtype, dh, H, G, users):
+    """2, 6, 8 and 4 query heads a key head: blocks of 64 rows of 2 heads, or of 32 rows of 4."""
+    _compare(DT[dtype], _where(users), H, G, dh, seed=H)
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (2, 1), (2, 2), (4, 4), (3, 3)])
+def test_head_counts_and_many_blocks(H, G):
+    """1, 2, 4 and 3 heads (or pairs of heads): how blocks are dealt to the chip, with units left over."""
+    users = [(64 * u % 301, [(1 + 17 * u % 200, 64 * u % 301)]) for u in range(530 // H)]
+    _compare(torch.bfloat16, _where(users), H, G, 32, seed=3)
