@@ -226,3 +226,18 @@ def test_many_buckets(dtype, dh, R):
     q, k, v, do, rel = _inputs(dt, int(off[-1]), 2, 1, dh, R, seed=R + dh)
     worst = F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
     log(f"rel {dtype} d_h {dh} R {R}: {worst}")
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("L", [[5] * 100, [1] * 5 + [2] * 50, [20] * 50, [128, 100, 64, 33], [2] * 600],
+                         ids=["fives", "ones_and_twos", "twenties", "one_block", "wide_blocks"])
+def test_bias_gradient_of_short_sequences(dh, L):
+    """Rows that see few keys: their dS nearly cancels, so D may not carry the
+    rounding of a bf16 output. Bound: that of the same values in fp32, and the
+    rounding of the result."""
+    off = _off(L)
+    q, k, v, do, rel = _inputs(torch.bfloat16, int(off[-1]), 2, 1, dh, 16, seed=dh + len(L))
+    got = _step(q, k, v, rel, off, do)
+    want = F.attention(*(t.float() for t in (q, k, v)), F.sequences(off), rel.float(), dout=do.float())
+    ref, bound = want["drel"]
+    F.check({"drel": got["drel"]}, {"drel": (ref, bound + F.unit(torch.bfloat16) * ref.abs())})
