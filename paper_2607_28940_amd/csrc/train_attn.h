@@ -64,6 +64,7 @@ struct TrainArgs {
   const TrainGroup* groups;
   int32_t n_groups, H, G;  // H query heads, G key heads
   int32_t n_units, q_chunk, k_units, k_chunk;  // units of either side and their place_chunk
+  const uint32_t *q_order, *k_order;  // units by work, group + 65536 local; null: group after group
   HeadRows q, k, v, o, dO, dq, dk, dv;
   float* lse;           // [H][lse_ld], natural logarithm
   int64_t lse_ld;
@@ -687,6 +688,20 @@ __device__ __forceinline__ void place(int chunk, int heads, int& unit, int& head
     head = b % heads;
     unit = b / heads;
   }
+}
+
+// The unit's group, and its number within it.
+template <bool KEYS>
+__device__ __forceinline__ TrainGroup group_of(const TrainArgs& a, int unit, int lane, int& local) {
+  const uint32_t* const order = KEYS ? a.k_order : a.q_order;
+  if (order) {
+    const uint32_t x = order[unit];
+    local = x >> 16;
+    return a.groups[x & 0xffff];
+  }
+  const TrainGroup g = a.groups[find_group<KEYS>(a.groups, a.n_groups, unit, lane)];
+  local = unit - (KEYS ? g.unit_k : g.unit_q);
+  return g;
 }
 
 // Lets a kernel use more than 64 KB of LDS a block: remembers the most that it

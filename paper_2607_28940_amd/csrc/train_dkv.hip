@@ -61,8 +61,9 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
   place(a.k_chunk, a.G, unit, hk);
   if (unit >= a.k_units) return;
   const int per = a.H / a.G;
-  const TrainGroup g = a.groups[find_group<true>(a.groups, a.n_groups, unit, lane)];
-  const int parts = g.parts_k, local = unit - g.unit_k, part = local % parts, kblk = local / parts;
+  int local;
+  const TrainGroup g = group_of<true>(a, unit, lane, local);
+  const int parts = g.parts_k, part = local % parts, kblk = local / parts;
   const int k_first = kblk * ROWS, k_wave = k_first + (NARROW ? 0 : wave * 32), key = k_wave + l32;
   lds_char* const bufs = smem + (NARROW ? wave * 2 * BUFS * TB : 0);
   lds_float* const stat = stats + (NARROW ? wave * 6 * QT : 0);

@@ -48,9 +48,10 @@ __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_
   if (unit >= a.n_units) return;
   h0 <<= pack;
   const int h = h0 + (wave >> (2 - pack)), w_row = NARROW ? 0 : 32 * (wave & ((4 >> pack) - 1));
-  const TrainGroup g = a.groups[find_group<false>(a.groups, a.n_groups, unit, lane)];
+  int local;
+  const TrainGroup g = group_of<false>(a, unit, lane, local);
   const int parts = g.parts_q, blocks = (g.nq + ROWS - 1) / ROWS;
-  const int local = unit - g.unit_q, part = local % parts;
+  const int part = local % parts;
   // a group's last rows see the most keys (later events have longer prefixes): first
   const int qb = blocks - 1 - local / parts;
   const int q_first = qb * ROWS;

@@ -220,3 +220,11 @@ def test_head_counts_and_many_blocks(H, G):
     """1, 2, 4 and 3 heads (or pairs of heads): how blocks are dealt to the chip, with units left over."""
     users = [(64 * u % 301, [(1 + 17 * u % 200, 64 * u % 301)]) for u in range(530 // H)]
     _compare(torch.bfloat16, _where(users), H, G, 32, seed=3)
+
+
+def test_more_blocks_than_are_sorted():
+    r = np.random.default_rng(5)
+    users = [(int(r.integers(0, 9)), []) for _ in range(4500)]
+    users = [(n, [(int(r.integers(1, 3)), int(r.integers(0, n + 1)))]) for n, _ in users]
+    users[2000] = (300, [(140, 299), (3, 7)])
+    _compare(torch.bfloat16, _where(users), 1, 1, 32, seed=2)

@@ -241,3 +241,11 @@ def test_bias_gradient_of_short_sequences(dh, L):
     want = F.attention(*(t.float() for t in (q, k, v)), F.sequences(off), rel.float(), dout=do.float())
     ref, bound = want["drel"]
     F.check({"drel": got["drel"]}, {"drel": (ref, bound + F.unit(torch.bfloat16) * ref.abs())})
+
+
+def test_more_blocks_than_are_sorted():
+    L = [1 + i % 3 for i in range(4300)]
+    L[777] = 400
+    off = _off(L)
+    q, k, v, do, rel = _inputs(torch.bfloat16, int(off[-1]), 1, 1, 32, 9, seed=4)
+    F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
