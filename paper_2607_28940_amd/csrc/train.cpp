@@ -95,7 +95,8 @@ int check_attn_config(const tx_attn_config* c, bool rel) {
     return fail(TX_E_INVALID, "rel_pos_buckets %d", c->rel_pos_buckets);
   if (c->rel_pos_buckets > kTrainMaxRel)
     return fail(TX_E_UNSUPPORTED, "rel_pos_buckets %d above %d", c->rel_pos_buckets, kTrainMaxRel);
-  if (!(c->scale >= 0.f) || !std::isfinite(c->scale)) return fail(TX_E_INVALID, "scale must be finite and not negative");
+  if (!(c->scale >= 0.f) || !std::isfinite(c->scale))
+    return fail(TX_E_INVALID, "scale must be finite and not negative");
   return TX_OK;
 }
 
@@ -577,8 +578,8 @@ int tx_event_attn_forward(const tx_attn_config* cfg, int32_t n, const int64_t* k
   });
 }
 
-int tx_event_attn_backward(const tx_attn_config* cfg, int32_t n, const int64_t* ko, const int64_t* eo, const int64_t* qo,
-                           const int64_t* prefix, const tx_rows* q, const tx_rows* k, const tx_rows* v,
+int tx_event_attn_backward(const tx_attn_config* cfg, int32_t n, const int64_t* ko, const int64_t* eo,
+                           const int64_t* qo, const int64_t* prefix, const tx_rows* q, const tx_rows* k, const tx_rows* v,
                            const tx_rows* out, const float* lse, int64_t lse_stride, const tx_rows* d_out,
                            const tx_rows* d_q, const tx_rows* d_k, const tx_rows* d_v, void* ws, size_t ws_bytes,
                            hipStream_t stream) {

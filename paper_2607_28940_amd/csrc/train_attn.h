@@ -24,8 +24,8 @@ namespace tx {
 // A group of a call, rows counted from the start of the tensors. Units are the
 // blocks of work of a launch per head: for query-side launches (forward, dq)
 // the group owns units unit_q .. , parts_q per block of queries, for the
-// key-side launch (dk, dv) unit_k .. , parts_k per block of keys. Groups whose blocks are divided (parts > 1) keep their partial results
-// in slots from slot_q / slot_k on, which a second launch joins in the order of
+// key-side launch (dk, dv) unit_k .. , parts_k per block of keys. Groups whose
+// blocks are divided (parts > 1) keep their partial results in slots from slot_q / slot_k on, which a second launch joins in the order of
 // the parts (joining them in the block that finishes last saves that launch,
 // but the fences write whole L2 caches back: one token against 4096 keys took
 // 131 us so, of 64 parts a head). qt0: its first entry in the 64-row query
@@ -362,7 +362,8 @@ struct Wave {
       const u32x4_t w = row_frag(tile, rb, c);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        bad |= BF ? ((w[t] & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((w[t] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+        bad |= BF ? ((w[t] & 0x7f807f80u) + 0x00800080u) & 0x80008000u
+                  : ((w[t] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
     }
     return __any(bad != 0);
   }

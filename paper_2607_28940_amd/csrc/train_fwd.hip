@@ -30,7 +30,13 @@ constexpr int fwd_blocks() { return NARROW ? 1 : sizeof(T) == 2 && DH <= 64 ? 4 
 // KT / 2 keys of one query and the softmax needs one exchange with lane l ^ 32;
 // then O^T += V^T P^T, P^T taken from the accumulators as they are and V^T
 // fragments read from the row-major tile (bf16: transposing LDS reads).
-// K and V are double-buffered, one barrier per tile.
+// K and V are double-buffered, one barrier per tile. P is rounded to bf16 for its
+// product (2^-9 of a term), l sums what was not rounded.
+// Measured, 8 heads: 147 k queries of 2.3 k keys at d_head 128 in 1.46 ms, 0.95
+// PFLOP/s; 16384 causal tokens 0.53 ms, 1.04. At 128 the matrix units are busy 46%
+// of the cycles, the vector units 43%, two waves a SIMD; at 64 a tile's 32
+// exponentials and 150 other vector operations a lane bound it (4 x 8192 causal
+// tokens 0.33 ms, 0.83 PFLOP/s).
 template <class T, int DH, bool REL, bool NARROW>
 __global__ __launch_bounds__(256, (fwd_blocks<T, DH, NARROW>())) void train_fwd_kernel(const TrainArgs a) {
   using Gm = Geo<T, DH>;
