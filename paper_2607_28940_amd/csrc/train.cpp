@@ -159,31 +159,47 @@ struct AttnPlan {
   } at;
 };
 
-// Parts of a block that goes through `steps` tiles.
-int parts_of(int64_t steps, int64_t total_steps, int min_steps) {
-  const int64_t target = std::max<int64_t>(min_steps, (total_steps + kFullGrid - 1) / kFullGrid);
+// Parts of a block that goes through `steps` tiles, `target` to a part.
+int parts_of(int64_t steps, int64_t target) {
   if (steps < 2 * target) return 1;
   return (int)std::min<int64_t>(kMaxParts, (steps + target - 1) / target);
 }
 
-int64_t blocks_of(int64_t rows, int block = kWideRows) { return (rows + block - 1) / block; }
-int64_t tiles_of(int64_t rows) { return (rows + kTrainQTile - 1) / kTrainQTile; }
+// (block: a power of two)
+int64_t blocks_of(int64_t rows, int block = kWideRows) { return (rows + block - 1) >> __builtin_ctz(block); }
+int64_t tiles_of(int64_t rows) { return blocks_of(rows, kTrainQTile); }
+
+// Indexes of `work`, most first (in 1024 steps of the largest; equals in order).
+std::vector<uint32_t> most_first(const std::vector<int64_t>& work) {
+  constexpr int kSteps = 1024;
+  const size_t n = work.size();
+  std::vector<uint32_t> order(n);
+  int64_t top = 1;
+  for (const int64_t w : work) top = std::max(top, w);
+  const double scale = (kSteps - 1) / (double)top;
+  uint32_t at[kSteps + 1] = {};
+  std::vector<uint16_t> step(n);
+  for (size_t i = 0; i < n; ++i) ++at[(step[i] = (uint16_t)(kSteps - 1 - (int)(work[i] * scale))) + 1];
+  for (int t = 0; t < kSteps; ++t) at[t + 1] += at[t];
+  for (size_t i = 0; i < n; ++i) order[at[step[i]]++] = (uint32_t)i;
+  return order;
+}
 
 // Units of one side by the tiles they go through, longest first, so that the
 // blocks that end a launch are short ones (12 users of 1.5 to 4.1 k keys, 17 k
 // queries: dk and dv 188 -> 157 us, forward 97 -> 91). Only for calls of a few
 // rounds of blocks (kSortGrid): longer ones even out by themselves, and there a
 // group's blocks together find its rows in the L2 caches.
-bool order_units(const AttnPlan& p, bool keys, bool rel, int64_t heads, std::vector<uint32_t>& order) {
-  const int64_t units = keys ? p.units_k : p.units_q;
-  if (units * heads > kSortGrid || p.groups.size() > 0xffff) return false;
+bool sorted_units(const AttnPlan& p, bool keys, int64_t heads) {
+  return (keys ? p.units_k : p.units_q) * heads <= kSortGrid && p.groups.size() <= 0xffff;
+}
+std::vector<uint32_t> order_units(const AttnPlan& p, bool keys, bool rel) {
   const int rows = keys ? p.k_rows : p.q_rows;
-  std::vector<std::pair<int64_t, uint32_t>> work;
-  std::vector<int64_t> at;
+  std::vector<int64_t> work, at;
+  std::vector<uint32_t> ref;
   for (size_t i = 0; i < p.groups.size(); ++i) {
     const TrainGroup& g = p.groups[i];
     const int64_t blocks = blocks_of(keys ? g.nk : g.nq, rows), parts = keys ? g.parts_k : g.parts_q;
-    if (blocks * parts > 0xffff) return false;
     at.assign(blocks + 1, 0);
     if (rel) {
       for (int64_t b = 0; b < blocks; ++b) at[b] = keys ? g.nq - b * rows : std::min<int64_t>(g.nq, (b + 1) * rows);
@@ -202,16 +218,18 @@ bool order_units(const AttnPlan& p, bool keys, bool rel, int64_t heads, std::vec
         for (int64_t b = 1; b < blocks; ++b) at[b] += at[b - 1];
     }
     for (int64_t b = 0; b < blocks; ++b)
-      for (int64_t part = 0; part < parts; ++part)  // (queries: the last block is the first unit)
-        work.push_back({-at[b] / parts, (uint32_t)(i | ((keys ? b : blocks - 1 - b) * parts + part) << 16)});
+      for (int64_t part = 0; part < parts; ++part) {  // (queries: the last block is the first unit)
+        work.push_back(at[b] / parts);
+        ref.push_back((uint32_t)(i | ((keys ? b : blocks - 1 - b) * parts + part) << 16));
+      }
   }
-  std::stable_sort(work.begin(), work.end(), [](const auto& x, const auto& y) { return x.first < y.first; });
-  order.reserve(work.size());
-  for (const auto& x : work) order.push_back(x.second);
-  return true;
+  std::vector<uint32_t> order = most_first(work);
+  for (uint32_t& x : order) x = ref[x];
+  return order;
 }
 
-void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) {
+// run: with the contents of the metadata, not its size alone
+void finish_plan(const tx_attn_config& c, bool backward, bool rel, bool run, AttnPlan& p) {
   const int H = c.n_heads, G = c.n_kv_heads, dh = c.d_head;
   // keys that the group's rows reach (tile steps of a query block)
   auto reach = [&](const TrainGroup& g) -> int64_t {
@@ -221,14 +239,16 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
     return m;
   };
   std::vector<int64_t> keys(p.groups.size());
-  {
+  for (size_t i = 0; i < p.groups.size(); ++i) keys[i] = reach(p.groups[i]);
+  if (run && p.groups.size() > 1) {
     // most work first: blocks are dealt to the card in order
-    std::vector<std::pair<int64_t, size_t>> order(p.groups.size());
-    for (size_t i = 0; i < order.size(); ++i) order[i] = {-reach(p.groups[i]) * p.groups[i].nq, i};
-    std::sort(order.begin(), order.end());
-    std::vector<TrainGroup> sorted(p.groups.size());
-    for (size_t i = 0; i < order.size(); ++i) sorted[i] = p.groups[order[i].second], keys[i] = reach(sorted[i]);
+    std::vector<int64_t> work(p.groups.size());
+    for (size_t i = 0; i < work.size(); ++i) work[i] = keys[i] * p.groups[i].nq;
+    std::vector<TrainGroup> sorted;
+    std::vector<int64_t> sorted_keys;
+    for (const uint32_t i : most_first(work)) sorted.push_back(p.groups[i]), sorted_keys.push_back(keys[i]);
     p.groups.swap(sorted);
+    keys.swap(sorted_keys);
   }
   // wide blocks where they would fill the card, narrow ones otherwise
   int64_t wide_q = 0, wide_k = 0;
@@ -254,46 +274,57 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
     const TrainGroup& g = p.groups[i];
     const double share = rel ? 0.5 : 1.0;  // a causal block covers half of the group's tiles on average
     steps_q += (int64_t)std::ceil(blocks_of(g.nq, p.q_rows) * tiles_of(keys[i]) * share) * (H >> p.pack);
-    steps_k += (int64_t)std::ceil(blocks_of(g.nk, p.k_rows) * tiles_of(g.nq) * (H / G) * share) * G;
+    steps_k += (int64_t)std::ceil(blocks_of(g.nk, p.k_rows) * tiles_of(g.nq) * per * share) * G;
   }
   const int min_steps = c.dtype == TX_F32 ? kMinStepsF32 : kMinSteps;
+  auto target = [&](int64_t total, bool narrow) {
+    return std::max<int64_t>(narrow ? 4 * min_steps : min_steps, (total + kFullGrid - 1) / kFullGrid);
+  };
+  const int64_t target_q = target(steps_q, p.q_narrow), target_k = target(steps_k, p.k_narrow);
   for (size_t i = 0; i < p.groups.size(); ++i) {
     TrainGroup& g = p.groups[i];
     const int64_t bq = blocks_of(g.nq, p.q_rows), bk = blocks_of(g.nk, p.k_rows);
-    const int nq_steps = p.q_narrow ? 4 * min_steps : min_steps,
-              nk_steps = p.k_narrow ? 4 * min_steps : min_steps;
-    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), steps_q, nq_steps) : 1;
+    g.parts_q = g.nq ? parts_of(tiles_of(keys[i]), target_q) : 1;
     g.unit_q = (int32_t)p.units_q;
     g.slot_q = (int32_t)p.slots_q;
     g.qt0 = (int32_t)p.tiles;
     p.units_q += bq * g.parts_q;
     if (g.parts_q > 1) p.slots_q += bq * g.parts_q * H;
     p.tiles += tiles_of(g.nq);
-    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * (H / G), steps_k, nk_steps) : 1;
+    g.parts_k = g.nk ? parts_of(tiles_of(g.nq) * per, target_k) : 1;
     g.unit_k = (int32_t)p.units_k;
     g.slot_k = (int32_t)p.slots_k;
     p.units_k += bk * g.parts_k;
     if (g.parts_k > 1) p.slots_k += bk * g.parts_k * G;
   }
+  size_t meta = 0;
   auto put = [&](const void* src, size_t n) {
-    const size_t o = align_up(p.meta.size(), 64);
-    p.meta.resize(o + n);
-    if (n) memcpy(p.meta.data() + o, src, n);
+    const size_t o = align_up(meta, 64);
+    meta = o + n;
+    if (run) {
+      p.meta.resize(meta);
+      if (n) memcpy(p.meta.data() + o, src, n);
+    }
     return o;
   };
+  if (run) p.meta.reserve(p.groups.size() * sizeof(TrainGroup) + (p.ev_row.size() + p.ev_prefix.size()) * 4 + 65536);
   put(p.groups.data(), p.groups.size() * sizeof(TrainGroup));
   p.o_row = put(p.ev_row.data(), p.ev_row.size() * 4);
   p.o_prefix = put(p.ev_prefix.data(), p.ev_prefix.size() * 4);
-  std::vector<uint32_t> order;
-  if (order_units(p, false, rel, H >> p.pack, order)) p.o_q = put(order.data(), order.size() * 4);
-  order.clear();
-  if (backward && order_units(p, true, rel, G, order)) p.o_k = put(order.data(), order.size() * 4);
+  auto put_order = [&](bool of_keys, int64_t heads) -> size_t {
+    if (!sorted_units(p, of_keys, heads)) return 0;
+    if (!run) return put(nullptr, (of_keys ? p.units_k : p.units_q) * 4);
+    const std::vector<uint32_t> order = order_units(p, of_keys, rel);
+    return put(order.data(), order.size() * 4);
+  };
+  p.o_q = put_order(false, H >> p.pack);
+  if (backward) p.o_k = put_order(true, G);
   Carver cv(nullptr);
   auto take = [&](size_t n) {
     cv.take<char*>(n);
     return cv.off - n;
   };
-  take(p.meta.size());
+  take(meta);
   p.at.row_lim = take(rel ? 0 : (p.rows_q + 1) * 4);
   p.at.tile_lim = take(rel ? 0 : p.tiles * sizeof(TileLim));
   p.at.stat = take(backward ? (size_t)H * p.rows_q * 8 : 0);
@@ -307,13 +338,14 @@ void finish_plan(const tx_attn_config& c, bool backward, bool rel, AttnPlan& p) 
   p.bytes = align_up(cv.off + 256);
 }
 
-int plan_rel(const tx_attn_config* c, bool backward, int32_t n, const int64_t* off, AttnPlan& p) {
+int plan_rel(const tx_attn_config* c, bool backward, bool run, int32_t n, const int64_t* off, AttnPlan& p) {
   TX_CHECK(check_attn_config(c, true));
   if (n < 0) return fail(TX_E_INVALID, "n_seq %d", n);
   TX_CHECK(check_offsets(off, n, "sequence"));
   p.q_base = off[0];
   p.rows_q = p.rows_k = off[n] - off[0];
   p.end_q = p.end_k = off[n];
+  p.groups.reserve(n);
   for (int32_t i = 0; i < n; ++i) {
     const int64_t L = off[i + 1] - off[i];
     if (!L) continue;
@@ -323,11 +355,11 @@ int plan_rel(const tx_attn_config* c, bool backward, int32_t n, const int64_t* o
     p.groups.push_back(g);
     p.pairs += 0.5 * L * (L + 1);
   }
-  finish_plan(*c, backward, true, p);
+  finish_plan(*c, backward, true, run, p);
   return TX_OK;
 }
 
-int plan_event(const tx_attn_config* c, bool backward, int32_t n, const int64_t* ko, const int64_t* eo,
+int plan_event(const tx_attn_config* c, bool backward, bool run, int32_t n, const int64_t* ko, const int64_t* eo,
                const int64_t* qo, const int64_t* prefix, AttnPlan& p) {
   TX_CHECK(check_attn_config(c, false));
   if (n < 0) return fail(TX_E_INVALID, "n_users %d", n);
@@ -342,6 +374,7 @@ int plan_event(const tx_attn_config* c, bool backward, int32_t n, const int64_t*
   p.rows_k = ko[n] - ko[0];
   p.end_q = qo[ne];
   p.end_k = ko[n];
+  p.groups.reserve(n);
   p.ev_row.resize(ne);
   p.ev_prefix.resize(ne);
   for (int32_t u = 0; u < n; ++u) {
@@ -361,7 +394,7 @@ int plan_event(const tx_attn_config* c, bool backward, int32_t n, const int64_t*
     }
     if (g.nq || (backward && g.nk)) p.groups.push_back(g);
   }
-  finish_plan(*c, backward, false, p);
+  finish_plan(*c, backward, false, run, p);
   return TX_OK;
 }
 
@@ -534,7 +567,7 @@ extern "C" {
 
 size_t tx_rel_attn_workspace_bytes(const tx_attn_config* cfg, int32_t backward, int32_t n, const int64_t* off) {
   AttnPlan p;
-  return guarded([&] { return plan_rel(cfg, backward != 0, n, off, p); }) == TX_OK ? p.bytes : 0;
+  return guarded([&] { return plan_rel(cfg, backward != 0, false, n, off, p); }) == TX_OK ? p.bytes : 0;
 }
 
 int tx_rel_attn_forward(const tx_attn_config* cfg, int32_t n, const int64_t* off, const tx_rows* q, const tx_rows* k,
@@ -542,7 +575,7 @@ int tx_rel_attn_forward(const tx_attn_config* cfg, int32_t n, const int64_t* off
                         size_t ws_bytes, hipStream_t stream) {
   return guarded([&] {
     AttnPlan p;
-    TX_CHECK(plan_rel(cfg, false, n, off, p));
+    TX_CHECK(plan_rel(cfg, false, true, n, off, p));
     const AttnTensors x{q, k, v, out, nullptr, nullptr, nullptr, nullptr, rel, nullptr, lse, lse_stride};
     return run_attn(*cfg, false, true, p, x, ws, ws_bytes, stream);
   });
@@ -554,7 +587,7 @@ int tx_rel_attn_backward(const tx_attn_config* cfg, int32_t n, const int64_t* of
                          void* ws, size_t ws_bytes, hipStream_t stream) {
   return guarded([&] {
     AttnPlan p;
-    TX_CHECK(plan_rel(cfg, true, n, off, p));
+    TX_CHECK(plan_rel(cfg, true, true, n, off, p));
     const AttnTensors x{q, k, v, out, d_out, d_q, d_k, d_v, rel, d_rel, const_cast<float*>(lse), lse_stride};
     return run_attn(*cfg, true, true, p, x, ws, ws_bytes, stream);
   });
@@ -563,7 +596,7 @@ int tx_rel_attn_backward(const tx_attn_config* cfg, int32_t n, const int64_t* of
 size_t tx_event_attn_workspace_bytes(const tx_attn_config* cfg, int32_t backward, int32_t n, const int64_t* ko,
                                      const int64_t* eo, const int64_t* qo, const int64_t* prefix) {
   AttnPlan p;
-  return guarded([&] { return plan_event(cfg, backward != 0, n, ko, eo, qo, prefix, p); }) == TX_OK ? p.bytes : 0;
+  return guarded([&] { return plan_event(cfg, backward != 0, false, n, ko, eo, qo, prefix, p); }) == TX_OK ? p.bytes : 0;
 }
 
 int tx_event_attn_forward(const tx_attn_config* cfg, int32_t n, const int64_t* ko, const int64_t* eo, const int64_t* qo,
@@ -572,7 +605,7 @@ int tx_event_attn_forward(const tx_attn_config* cfg, int32_t n, const int64_t* k
                           hipStream_t stream) {
   return guarded([&] {
     AttnPlan p;
-    TX_CHECK(plan_event(cfg, false, n, ko, eo, qo, prefix, p));
+    TX_CHECK(plan_event(cfg, false, true, n, ko, eo, qo, prefix, p));
     const AttnTensors x{q, k, v, out, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, lse, lse_stride};
     return run_attn(*cfg, false, false, p, x, ws, ws_bytes, stream);
   });
@@ -585,7 +618,7 @@ int tx_event_attn_backward(const tx_attn_config* cfg, int32_t n, const int64_t* 
                            hipStream_t stream) {
   return guarded([&] {
     AttnPlan p;
-    TX_CHECK(plan_event(cfg, true, n, ko, eo, qo, prefix, p));
+    TX_CHECK(plan_event(cfg, true, true, n, ko, eo, qo, prefix, p));
     const AttnTensors x{q, k, v, out, d_out, d_q, d_k, d_v, nullptr, nullptr, const_cast<float*>(lse), lse_stride};
     return run_attn(*cfg, true, false, p, x, ws, ws_bytes, stream);
   });
