@@ -311,8 +311,9 @@ int score_candidates_static(const tx_kv_cache* cache, int32_t n_req, const int32
  * its host arrays before it returns, never synchronises, allocates no device
  * memory and may be captured into a graph; calls that run at the same time need
  * workspaces of their own. The same inputs give the same bits, eager or
- * replayed. Checks and errors as above: TX_E_INVALID, TX_E_UNSUPPORTED and
- * TX_E_NOMEM (workspace too small) before anything is launched, TX_E_HIP. */
+ * replayed. Checks and errors as above: TX_E_INVALID, TX_E_UNSUPPORTED (types,
+ * sizes, more than 2^24 blocks of rows times heads) and TX_E_NOMEM (workspace too
+ * small) before anything is launched, TX_E_HIP. */
 
 typedef struct {
   int32_t dtype;           /* tx_dtype of every tensor but the fp32 statistics */

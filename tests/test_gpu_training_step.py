@@ -199,3 +199,53 @@ def test_two_captured_steps(dtype):
             _check(outs[i], *wants[i])
             for t in outs[i].values():
                 t.zero_()
+
+
+def test_steps_at_once_from_threads():
+    """Two threads, each with its stream and its batch, at the same time: nothing is shared between calls."""
+    import threading
+    steps = [Step(torch.bfloat16, seed=s, dh=dh) for s, dh in ((3, 32), (4, 64))]
+    wants = [_bounds(s) for s in steps]
+    own = [Own(s) for s in steps]
+    streams = [torch.cuda.Stream() for _ in own]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(streams[i]):
+                for _ in range(8):
+                    got[i].append(own[i].run())
+        except Exception as e:  # noqa: BLE001 (reported below)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for i in (0, 1):
+        for r in got[i]:
+            _check(r, *wants[i])
+
+
+def test_a_stream_that_is_not_the_current_one():
+    """stream=: the call runs there, after what it waits for there."""
+    s = Step(torch.float32, seed=6)
+    side = torch.cuda.Stream()
+    off = s.k_off
+    n = int(off[-1])
+    gen = torch.Generator().manual_seed(1)
+    src = torch.randn(n, 4, 32, generator=gen)
+    plain = T.rel_attention(src.cuda(), src.cuda(), src.cuda(), None, off)
+    torch.cuda.synchronize()
+    q = torch.zeros(n, 4, 32, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        q.copy_(src.pin_memory(), non_blocking=True)
+    out, lse = T.rel_attention(q, q, q, None, off, stream=side)
+    side.synchronize()
+    assert torch.equal(out, plain[0]) and torch.equal(lse, plain[1])
