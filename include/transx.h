@@ -341,7 +341,8 @@ typedef struct {
  * offsets[i+1]-1 (it may have none), and within it
  *   t_ij = scale q_i . k_j + rel[h][min(i - j, R - 1)]  for j <= i
  *   out_i = softmax_j(t_ij) v_j,  lse[h * lse_stride + row] = log sum_j exp t_ij
- * rel: device [n_heads][R] (null when R = 0). A bias of -1e30 or less masks its
+ * rel: device [n_heads][R] (null when R = 0), values up to 1e30 (logits are held
+ * in fp32, in base 2). A bias of -1e30 or less masks its
  * distances, whatever the keys and values there hold; a row with every distance
  * masked gives out 0 and lse -inf, and its gradients are 0. lse_stride >=
  * offsets[n_seq]. Rows outside the offsets are neither read nor written.

@@ -249,3 +249,20 @@ def test_more_blocks_than_are_sorted():
     off = _off(L)
     q, k, v, do, rel = _inputs(torch.bfloat16, int(off[-1]), 1, 1, 32, 9, seed=4)
     F.check(_step(q, k, v, rel, off, do), F.attention(q, k, v, F.sequences(off), rel, dout=do))
+
+
+def test_a_very_long_sequence():
+    """131 k tokens: rows from everywhere against the formula, and dv, whose sum over keys is that of dO."""
+    dt, L, dh = torch.bfloat16, 131072 + 77, 64
+    q, k, v, do, _ = _inputs(dt, L, 1, 1, dh, 0, seed=12)
+    got = _step(q, k, v, None, _off([L]), do)
+    rows = torch.tensor([0, 1, 63, 64, 4095, 4096, 50001, 65535, 65536, 100000, L - 78, L - 2, L - 1])
+    want = F.attention(q[rows.cuda()], k, v, [((0, len(rows)), (0, L), (rows + 1).numpy())], dout=do[rows.cuda()])
+    some = {n: got[n][rows.cuda()] for n in ("out", "dq")}
+    some["lse"] = got["lse"][:, rows.cuda()]
+    F.check(some, {n: want[n] for n in some})
+    u = F.unit(dt)
+    sums = got["dv"].double().sum(0) - do.double().sum(0)
+    # the probabilities' rounding (u each, they sum to 1 a row, and fp32 sums) and dv's own
+    bound = (u + (2 * L) * F.U32) * do.double().abs().sum(0) + u * got["dv"].double().abs().sum(0)
+    assert bool((sums.abs() <= bound).all())
